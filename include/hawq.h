@@ -2,11 +2,12 @@
  * hawq.h -- C interface of the MI355X (gfx950) integer-only inference kernels for
  * HAWQ-V3 ("Dyadic Neural Network Quantization").
  *
- * The library implements the inference-time arithmetic of the paper and nothing else:
- * low-bit integer convolution / matrix multiply with INT32 accumulation, INT32 bias add,
- * requantisation by a dyadic number b / 2^c (one integer multiply, one rounding right
- * shift; no floating point, no integer division), ReLU / clamp, the dyadic residual
- * addition and integer pooling.
+ * The library implements the inference-time arithmetic of the paper: low-bit integer convolution /
+ * matrix multiply with INT32 accumulation, INT32 bias add, requantisation by a dyadic number
+ * b / 2^c (one integer multiply, one rounding right shift; no floating point, no integer
+ * division), ReLU / clamp, the dyadic residual addition and integer pooling.  Beside it stand
+ * the operators of a language model served from 4-bit weights and a paged cache (second half:
+ * hawq_linear_w4, hawq_attn_*, hawq_cache_*), which compute in floating point.
  *
  * Conventions that hold for every entry point unless stated otherwise
  * -------------------------------------------------------------------
@@ -56,7 +57,8 @@ typedef enum {
     HAWQ_ERR_WORKSPACE = 8    /* caller's workspace is too small */
 } hawq_status;
 
-typedef enum { HAWQ_U8 = 0, HAWQ_S8 = 1, HAWQ_U4 = 2, HAWQ_S4 = 3, HAWQ_S32 = 4 } hawq_dtype;
+typedef enum { HAWQ_U8 = 0, HAWQ_S8 = 1, HAWQ_U4 = 2, HAWQ_S4 = 3, HAWQ_S32 = 4,
+               HAWQ_F16 = 5, HAWQ_BF16 = 6 /* only where an entry point names them: the language-model operators */ } hawq_dtype;
 
 /* One quantised convolution layer (all fields int32 so the struct has no padding). */
 typedef struct {
@@ -387,6 +389,130 @@ hawq_status hawq_forward_resnet_timed(const hawq_net *net, const void *x, int32_
 /* Static description of a step for reporting: multiply-accumulates and minimum HBM bytes
  * (input once + weights + parameters + output once + shortcut once) at batch N. */
 hawq_status hawq_net_step_cost(const hawq_net *net, int32_t N, int32_t step, double *macs, double *bytes);
+
+/* ---------------------------------------------------------------------------------------------
+ * Serving a language model from 4-bit weights and a paged cache.
+ *
+ * Activations are HAWQ_F16 or HAWQ_BF16 (one type per call, called T below); sums, softmax statistics and scales are
+ * computed in 32-bit floating point and a result is rounded once, to nearest even, when it is stored.  The conventions
+ * above hold: device pointers owned by the caller, no allocation, nothing kept, work only enqueued, errors are codes.
+ * Strides are in elements, the innermost axis is contiguous; a stride may exceed its axis (a slice of a
+ * wider tensor), and be 0 where a tensor that is only read is broadcast.
+ * Elements of T lie at even addresses, scales at multiples of four (HAWQ_ERR_UNSUPPORTED otherwise).  Lengths, tables and
+ * masks are device data: they are not checked on the host but bounded by the kernels, so that a wrong one gives a wrong
+ * result and no access outside the tensors described.
+ * ------------------------------------------------------------------------------------------- */
+
+/*
+ * Linear layer with 4-bit weights and one scale for every `group` consecutive weights of an output:
+ *   y[m,n] = sum_k x[m,k] * (q[n,k] - z[n, k / group]) * s[n, k / group]  (+ bias[n])
+ * w [N, K/2] packed as everywhere (element 2i in bits 0..3): HAWQ_S4 with zeros == NULL (z = 0), or HAWQ_U4 with zeros
+ * uint8 [N, groups], values 0..15; scales T [N, groups], groups = ceil(K / group); bias T [N] or NULL.
+ * x rows x_stride apart, y rows y_stride apart.  K even, group a positive multiple of 32 (the last group may be short).
+ * Made for the rows of a decoding step, a few to some tens: the weights are read once for every 64 rows of x.
+ * Any valid request is served; 16-byte aligned w and K a multiple of 32 read it in whole vectors.
+ */
+typedef struct {
+    int32_t M, N, K;
+    int32_t group;
+    int32_t x_dtype;               /* T: HAWQ_F16 | HAWQ_BF16 */
+    int32_t w_dtype;               /* HAWQ_S4 | HAWQ_U4 */
+    int64_t x_stride, y_stride;
+} hawq_linear_w4_desc;
+hawq_status hawq_linear_w4(const hawq_linear_w4_desc *desc, const void *x, const void *w, const void *scales, const uint8_t *zeros,
+                           const void *bias, void *y, void *stream);
+
+/*
+ * Causal attention over whole prompts, the sequences of a batch packed one behind the other:
+ *   y[i,h] = sum_j p_ij v[j, h / r],   p_i = softmax_j( scale * q[i,h] . k[j, h / r] ),   j of i's sequence, j <= i
+ * q, y [total, q_heads, head_dim], k, v [total, kv_heads, head_dim] of T with the strides given, r = q_heads / kv_heads.
+ * starts: int32 [n_seqs + 1], sequence b holds rows starts[b] .. starts[b+1] - 1 (empty ones allowed), starts[0] = 0 and
+ * starts[n_seqs] = total; rows outside every sequence are not written.  head_dim 1..256, q_heads a multiple of kv_heads.
+ * A row's result does not depend on keys and values after it, whatever they hold (infinities and NaN included); a row
+ * whose scores are all -infinity gives zeros.  Probabilities may be rounded to T before they meet the values.
+ * head_dim a multiple of 8 up to 128 with 16-byte aligned rows runs on the matrix cores.
+ */
+typedef struct {
+    int32_t n_seqs, total;
+    int32_t q_heads, kv_heads, head_dim;
+    int32_t dtype;                 /* T */
+    float scale;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, y_token, y_head;   /* strides */
+} hawq_attn_prompt_desc;
+hawq_status hawq_attn_prompt(const hawq_attn_prompt_desc *desc, const void *q, const void *k, const void *v, const int32_t *starts,
+                             void *y, void *stream);
+
+/*
+ * A paged cache of keys and of values, two tensors of one shape and layout: element (page, token, head, i) lies at
+ * page * page_stride + token * token_stride + head * head_stride + i.  dtype T, or HAWQ_S8 with scales float32
+ * [n_pages, page, kv_heads] (one for each token and head; value = code * scale).
+ */
+typedef struct {
+    int32_t n_pages, page;         /* pages, tokens of a page */
+    int32_t kv_heads, head_dim;
+    int32_t dtype;
+    int64_t page_stride, token_stride, head_stride;
+} hawq_cache_desc;
+
+/*
+ * Attention of the drafted tokens of a batch of requests over their cached tokens and over one another:
+ * row t of request b attends to the cached tokens 0 .. cached[b] - 1 of b (page i of them is table[b * table_stride + i])
+ * and to those drafted tokens j of b whose bit j is set in mask[t] -- its ancestors in a tree of drafts and itself.
+ * mask == NULL: every drafted token up to and including itself.  A row that sees nothing gives zeros.
+ * q, y [total, q_heads, head_dim], k, v [total, kv_heads, head_dim] of T hold the drafted tokens of all requests, starts
+ * as in hawq_attn_prompt; one drafted token per request is ordinary decoding.  The drafts' keys and values need not be in
+ * the cache (hawq_cache_store puts the accepted ones there).  max_drafts (1..64) and max_cached bound the requests'
+ * numbers of drafts and of cached tokens; what is beyond them, or beyond table_stride pages, is not seen (nor a row beyond
+ * them written), nor is a page whose number is outside the cache.  k_scales / v_scales: with a HAWQ_S8 cache only, else NULL.
+ * Values that a row does not see do not change it, whatever they hold; a row whose scores are all -infinity gives zeros.
+ * Probabilities (times the value's scale) may be rounded to T before they meet the values.  workspace: device memory of
+ * hawq_attn_tree_workspace_bytes(desc) bytes (0 for an invalid desc), 16-byte aligned, scratch for partial sums where a
+ * long cache is shared out to several workgroups.
+ */
+typedef struct {
+    hawq_cache_desc cache;
+    int32_t n_seqs, total;
+    int32_t max_drafts, max_cached;
+    int32_t q_heads;
+    int32_t dtype;                 /* T */
+    int32_t table_stride;
+    float scale;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, y_token, y_head;   /* strides */
+} hawq_attn_tree_desc;
+size_t hawq_attn_tree_workspace_bytes(const hawq_attn_tree_desc *desc);
+hawq_status hawq_attn_tree(const hawq_attn_tree_desc *desc, const void *q, const void *k, const void *v, const int32_t *starts,
+                           const uint64_t *mask, const void *k_cache, const void *v_cache, const float *k_scales, const float *v_scales,
+                           const int32_t *table, const int32_t *cached, void *y, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Room in the cache for the fresh tokens of a batch of requests, in one launch: request b holds cached[b] tokens and gets
+ * fresh[b] more (negative numbers count as 0).  Its first ceil(cached / page) pages are in its row of the block table
+ * [n_seqs, table_stride]; the pages up to ceil((cached + fresh) / page), as far as the row reaches, are taken in order
+ * of the requests from free_pages [n_free] and written to the table (-1 where the list is used up).
+ *   starts  int32 [n_seqs + 1]: fresh tokens of the requests before, and their total
+ *   slots   int64 [n_slots]: page * tokens-of-a-page + place of every fresh token, packed by starts; -1 for a token
+ *           without a page and for entries past the total
+ *   counts  int32 [2]: the total of fresh tokens; the pages taken (more than n_free: the list was too short)
+ * Totals must stay below 2^31.  The inputs and the held part of the table are not changed, so a call can be repeated.
+ */
+hawq_status hawq_cache_plan(int32_t n_seqs, int32_t page, int32_t table_stride, int32_t n_free, int64_t n_slots, const int32_t *cached,
+                            const int32_t *fresh, const int32_t *free_pages, int32_t *table, int32_t *starts, int64_t *slots,
+                            int32_t *counts, void *stream);
+
+/*
+ * New rows of keys and values to their slots: row t of k, v [total, kv_heads, head_dim] (T, strides given) goes to token
+ * slots[t] % page of page slots[t] / page; a slot outside the cache (as -1) skips the row.  No two rows may share a slot.
+ * A HAWQ_S8 cache gets, for each token and head, scale = max|x| / 127 and codes rint(x / scale), ties to even, computed in
+ * float32 (scale 0 and codes 0 for a row of zeros); a row with an infinity or a NaN gets the scale NaN.
+ */
+typedef struct {
+    hawq_cache_desc cache;
+    int32_t total;
+    int32_t dtype;                 /* T */
+    int64_t k_token, k_head, v_token, v_head;   /* strides */
+} hawq_cache_store_desc;
+hawq_status hawq_cache_store(const hawq_cache_store_desc *desc, const void *k, const void *v, const int64_t *slots, void *k_cache,
+                             void *v_cache, float *k_scales, float *v_scales, void *stream);
 
 /* Measurement hook for tile-shape sweeps: 0 = the built-in heuristic (default), 1..3 = force one of the
  * matrix-core kernel's workgroup tiles (128x128 as four waves, 64x128, 64x64 channels x pixels) for every

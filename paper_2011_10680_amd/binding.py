@@ -10,7 +10,7 @@ import os
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libhawq.so")
 
-U8, S8, U4, S4, S32 = 0, 1, 2, 3, 4
+U8, S8, U4, S4, S32, F16, BF16 = 0, 1, 2, 3, 4, 5, 6
 _STATUS_NAMES = {0: "HAWQ_OK", 1: "HAWQ_ERR_NULL", 2: "HAWQ_ERR_SHAPE", 3: "HAWQ_ERR_DTYPE", 4: "HAWQ_ERR_RANGE",
                  5: "HAWQ_ERR_OVERFLOW", 6: "HAWQ_ERR_UNSUPPORTED", 7: "HAWQ_ERR_DEVICE", 8: "HAWQ_ERR_WORKSPACE"}
 
@@ -42,6 +42,31 @@ class ConcatBranch(ctypes.Structure):
 class LayerInfo(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 24)] + [(n, ctypes.c_int32) for n in
                 ("C", "K", "R", "S", "stride", "pad", "H", "W", "P", "Q", "has_residual", "is_ds")]
+
+
+_ROWS = lambda *names: [("%s_%s" % (n, w), ctypes.c_int64) for n in names for w in ("token", "head")]
+
+
+class LinearW4Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("M", "N", "K", "group", "x_dtype", "w_dtype")] + [("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64)]
+
+
+class AttnPromptDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "total", "q_heads", "kv_heads", "head_dim", "dtype")] + [("scale", ctypes.c_float)] + _ROWS("q", "k", "v", "y")
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page", "kv_heads", "head_dim", "dtype")] + [(n, ctypes.c_int64) for n in
+                ("page_stride", "token_stride", "head_stride")]
+
+
+class AttnTreeDesc(ctypes.Structure):
+    _fields_ = [("cache", CacheDesc)] + [(n, ctypes.c_int32) for n in ("n_seqs", "total", "max_drafts", "max_cached", "q_heads", "dtype", "table_stride")] + [
+                ("scale", ctypes.c_float)] + _ROWS("q", "k", "v", "y")
+
+
+class CacheStoreDesc(ctypes.Structure):
+    _fields_ = [("cache", CacheDesc), ("total", ctypes.c_int32), ("dtype", ctypes.c_int32)] + _ROWS("k", "v")
 
 
 _lib = None
@@ -118,6 +143,18 @@ def load_library():
     lib.hawq_tune_set_split.argtypes = [i32]
     lib.hawq_tune_set_fusion.restype = None
     lib.hawq_tune_set_fusion.argtypes = [i32]
+    lib.hawq_linear_w4.restype = ctypes.c_int
+    lib.hawq_linear_w4.argtypes = [ctypes.POINTER(LinearW4Desc)] + [vp] * 7
+    lib.hawq_attn_prompt.restype = ctypes.c_int
+    lib.hawq_attn_prompt.argtypes = [ctypes.POINTER(AttnPromptDesc)] + [vp] * 6
+    lib.hawq_attn_tree_workspace_bytes.restype = sz
+    lib.hawq_attn_tree_workspace_bytes.argtypes = [ctypes.POINTER(AttnTreeDesc)]
+    lib.hawq_attn_tree.restype = ctypes.c_int
+    lib.hawq_attn_tree.argtypes = [ctypes.POINTER(AttnTreeDesc)] + [vp] * 13 + [sz, vp]
+    lib.hawq_cache_plan.restype = ctypes.c_int
+    lib.hawq_cache_plan.argtypes = [i32] * 4 + [i64] + [vp] * 8
+    lib.hawq_cache_store.restype = ctypes.c_int
+    lib.hawq_cache_store.argtypes = [ctypes.POINTER(CacheStoreDesc)] + [vp] * 8
     lib.hawq_status_string.restype = ctypes.c_char_p
     lib.hawq_status_string.argtypes = [ctypes.c_int]
     _lib = lib
@@ -257,6 +294,36 @@ def hawq_concat_dyadic(n_pixels, branches, y_dt, y_lo, y_hi, y, stream=None):
         arr[i].K, arr[i].dtype = b.numel(), dt
     _check(load_library().hawq_concat_dyadic(n_pixels, len(branches), arr, y_dt, y_lo, y_hi, _p(y), _stream(stream)),
            "hawq_concat_dyadic")
+
+
+def hawq_linear_w4(desc, x, w, scales, zeros, bias, y, stream=None):
+    _check(load_library().hawq_linear_w4(ctypes.byref(desc), _p(x), _p(w), _p(scales), _p(zeros), _p(bias), _p(y), _stream(stream)), "hawq_linear_w4")
+
+
+def hawq_attn_prompt(desc, q, k, v, starts, y, stream=None):
+    _check(load_library().hawq_attn_prompt(ctypes.byref(desc), _p(q), _p(k), _p(v), _p(starts), _p(y), _stream(stream)), "hawq_attn_prompt")
+
+
+def hawq_attn_tree_workspace_bytes(desc):
+    return int(load_library().hawq_attn_tree_workspace_bytes(ctypes.byref(desc)))
+
+
+def hawq_attn_tree(desc, q, k, v, starts, mask, k_cache, v_cache, k_scales, v_scales, table, cached, y, workspace, stream=None):
+    """workspace: a tensor of at least hawq_attn_tree_workspace_bytes(desc) bytes, or None where that is 0."""
+    _check(load_library().hawq_attn_tree(ctypes.byref(desc), _p(q), _p(k), _p(v), _p(starts), _p(mask), _p(k_cache), _p(v_cache), _p(k_scales), _p(v_scales),
+                                          _p(table), _p(cached), _p(y), _p(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                          _stream(stream)), "hawq_attn_tree")
+
+
+def hawq_cache_plan(cached, fresh, page, free_pages, table, starts, slots, counts, stream=None):
+    """Sizes are taken from the tensors: requests from cached, the table's row from its second axis, free pages and slots from theirs."""
+    _check(load_library().hawq_cache_plan(cached.numel(), page, table.shape[1], free_pages.numel(), slots.numel(), _p(cached), _p(fresh), _p(free_pages), _p(table),
+                                           _p(starts), _p(slots), _p(counts), _stream(stream)), "hawq_cache_plan")
+
+
+def hawq_cache_store(desc, k, v, slots, k_cache, v_cache, k_scales, v_scales, stream=None):
+    _check(load_library().hawq_cache_store(ctypes.byref(desc), _p(k), _p(v), _p(slots), _p(k_cache), _p(v_cache), _p(k_scales), _p(v_scales), _stream(stream)),
+           "hawq_cache_store")
 
 
 def hawq_tune_set_tile(tile):

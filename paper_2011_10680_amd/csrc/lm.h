@@ -1,0 +1,99 @@
+// Internal declarations of the language-model operators: element types, argument blocks, launchers (gfx950 only).
+#pragma once
+#include "common.h"
+#include "fastdiv.h"
+
+namespace hawq {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+
+// The activations' type T: its name for the matrix instructions and how a float is rounded to it (nearest even).
+struct F16 {
+    typedef _Float16 elem;
+    typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 v4 __attribute__((ext_vector_type(4)));
+    typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ v4f mfma16(v8 a, v8 b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ v16f mfma32(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+struct BF16 {
+    typedef __bf16 elem;
+    typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 v4 __attribute__((ext_vector_type(4)));
+    typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ v4f mfma16(v8 a, v8 b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ v16f mfma32(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+
+struct LinearW4Args {
+    const void *x, *scales, *bias;
+    const uint8_t *w, *zeros;      // zeros == nullptr: signed weights
+    void *y;
+    int32_t M, N, K, group, groups;
+    int64_t x_stride, y_stride;
+    int32_t dtype;
+};
+
+struct AttnPromptArgs {
+    const void *q, *k, *v;
+    const int32_t *starts;
+    void *y;
+    int32_t n_seqs, total, q_heads, kv_heads, head_dim, dtype;
+    float scale;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, y_token, y_head;
+};
+
+struct CacheArgs {
+    void *k, *v;                   // the two tensors
+    float *ks, *vs;                // scales of an 8-bit cache
+    int32_t n_pages, page, dtype;
+    FastDiv by_page;
+    int64_t page_stride, token_stride, head_stride;
+};
+
+struct AttnTreeArgs {
+    const void *q, *k, *v;
+    const int32_t *starts, *table, *cached;
+    const uint64_t *mask;          // nullptr: a chain
+    void *y;
+    float *partial;                // workspace
+    CacheArgs cache;
+    int32_t n_seqs, total, max_drafts, max_cached, q_heads, kv_heads, head_dim, dtype, table_stride;
+    float scale;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, y_token, y_head;
+};
+
+struct CachePlanArgs {
+    int32_t n_seqs, page, table_stride, n_free;
+    int64_t n_slots;
+    const int32_t *cached, *fresh, *free_pages;
+    int32_t *table, *starts;
+    int64_t *slots;
+    int32_t *counts;
+};
+
+struct CacheStoreArgs {
+    const void *k, *v;
+    const int64_t *slots;
+    CacheArgs cache;
+    int32_t total, kv_heads, head_dim, dtype;
+    int64_t k_token, k_head, v_token, v_head;
+};
+
+hawq_status launch_linear_w4(const LinearW4Args &a, hipStream_t s);
+hawq_status launch_attn_prompt(const AttnPromptArgs &a, hipStream_t s);
+size_t attn_tree_workspace(const AttnTreeArgs &a);
+hawq_status launch_attn_tree(const AttnTreeArgs &a, hipStream_t s);
+hawq_status launch_cache_plan(const CachePlanArgs &a, hipStream_t s);
+hawq_status launch_cache_store(const CacheStoreArgs &a, hipStream_t s);
+
+// Rows [from, to) of sequence b, whatever the starts hold: inside [0, total) and not negative in number.
+__device__ __forceinline__ void sequence_rows(const int32_t *starts, int b, int total, int &from, int &to) {
+    from = min(max(starts[b], 0), total);
+    to = min(max(starts[b + 1], from), total);
+}
+
+}  // namespace hawq
