@@ -502,7 +502,7 @@ hawq_status hawq_cache_plan(int32_t n_seqs, int32_t page, int32_t table_stride, 
 /*
  * New rows of keys and values to their slots: row t of k, v [total, kv_heads, head_dim] (T, strides given) goes to token
  * slots[t] % page of page slots[t] / page; a slot outside the cache (as -1) skips the row.  No two rows may share a slot.
- * A HAWQ_S8 cache gets, for each token and head, scale = max|x| / 127 and codes rint(x / scale), ties to even, computed in
+ * A HAWQ_S8 cache gets, for each token and head, scale = max|x| * (1 / 127) and codes rint(x / scale), ties to even, computed in
  * float32 (scale 0 and codes 0 for a row of zeros); a row with an infinity or a NaN gets the scale NaN.
  */
 typedef struct {

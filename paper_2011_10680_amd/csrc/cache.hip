@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256) void cache_store(CacheStoreArgs a) {
         }
         for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
         finite = __all(finite);
-        const float scale = finite ? top / 127.f : __builtin_nanf("");
+        const float scale = finite ? top * (1.f / 127.f) : __builtin_nanf("");
         for (int i = lane; i < a.head_dim; i += 64) y[i] = scale > 0.f ? (int8_t)fminf(fmaxf(rintf((float)x[i] / scale), -127.f), 127.f) : 0;
         if (lane == 0) (blockIdx.y ? a.cache.vs : a.cache.ks)[slot * a.kv_heads + h] = scale;
     }

@@ -1,35 +1,222 @@
-// Linear layer with 4-bit weights and group scales.
+// Linear layer with 4-bit weights and a scale for each group of them, for the few rows of a decoding step.
+//
+//   y[m,n] = sum_g s[n,g] * ( sum_{k in g} x[m,k] u[n,k]  -  (16 + z[n,g]) * sum_{k in g} x[m,k] ),   u = 16 + nibble
+//
+// The matrix instruction takes 16 outputs x 32 weights from one register of packed nibbles per lane: a shift, and one
+// three-operand bit operation put two nibbles into the mantissas of two 16-bit floats of value 16 + nibble (exact in both
+// types; a signed nibble is its offset form with zero point 8), so a weight costs one vector operation and no conversion.
+// The zero point and the 16 leave through the sum of x over the group, which one product with a matrix of ones gives for
+// all outputs.  Group sums and totals are 32-bit; nothing is rounded before the result.
+//
+// Bound by the weights' bytes.  A wave reads 16 bytes per lane (four lanes cover 64 bytes of one output's row), and a 4 x 4
+// exchange between its quarters turns the four registers into four operands of 32 consecutive weights each, so that a group
+// of 32 has a matrix instruction of its own.  The waves of a workgroup take every W-th 128 weights of the same outputs and
+// add up in LDS: one output's reduction is shared by the whole workgroup, and few outputs still fill the chip.
 #include "lm.h"
 
 namespace hawq {
 
 namespace {
 
+template <class T> struct Nibbles;
+template <> struct Nibbles<F16> {            // 16 + u: 0x4C00 | u << 6
+    static constexpr uint32_t mask = 0x03C003C0u, base = 0x4C004C00u, sign = 0x02000200u, one = 0x3C003C00u;
+    template <int I> static __device__ __forceinline__ uint32_t shift(uint32_t d) { return I == 0 ? d << 6 : I == 1 ? d << 2 : I == 2 ? d >> 2 : d >> 6; }
+};
+template <> struct Nibbles<BF16> {           // 0x4180 | u << 3
+    static constexpr uint32_t mask = 0x00780078u, base = 0x41804180u, sign = 0x00400040u, one = 0x3F803F80u;
+    template <int I> static __device__ __forceinline__ uint32_t shift(uint32_t d) { return I == 0 ? d << 3 : I == 1 ? d >> 1 : I == 2 ? d >> 5 : d >> 9; }
+};
+
+// operand of eight weights: nibbles (0,4), (1,5), (2,6), (3,7)
 template <class T>
-__global__ __launch_bounds__(256) void linear_w4_any(LinearW4Args a) {
+__device__ __forceinline__ typename T::v8 expand(uint32_t d, uint32_t flip) {
+    v4u r;
+    r.x = (Nibbles<T>::template shift<0>(d) & Nibbles<T>::mask) ^ flip;
+    r.y = (Nibbles<T>::template shift<1>(d) & Nibbles<T>::mask) ^ flip;
+    r.z = (Nibbles<T>::template shift<2>(d) & Nibbles<T>::mask) ^ flip;
+    r.w = (Nibbles<T>::template shift<3>(d) & Nibbles<T>::mask) ^ flip;
+    return __builtin_bit_cast(typename T::v8, r);
+}
+
+// eight consecutive values of x in the same order
+template <class T>
+__device__ __forceinline__ typename T::v8 ordered(v4u d) {
+    v4u r;
+    r.x = __builtin_amdgcn_perm(d.z, d.x, 0x05040100u);
+    r.y = __builtin_amdgcn_perm(d.z, d.x, 0x07060302u);
+    r.z = __builtin_amdgcn_perm(d.w, d.y, 0x05040100u);
+    r.w = __builtin_amdgcn_perm(d.w, d.y, 0x07060302u);
+    return __builtin_bit_cast(typename T::v8, r);
+}
+
+// register j of the wave's quarter c <-> register c of its quarter j
+__device__ __forceinline__ void exchange_quarters(v4u &d) {
+    const v2u a = __builtin_amdgcn_permlane32_swap(d.x, d.z, false, false), b = __builtin_amdgcn_permlane32_swap(d.y, d.w, false, false);
+    const v2u e = __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false), f = __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
+    d.x = e.x; d.y = e.y; d.z = f.x; d.w = f.y;
+}
+
+// RT, MT: 16-output and 16-row tiles of a wave.  PIECES: parts of 128 weights with a scale of their own.  ALIGN: bytes the rows of w
+// are read in (16, 4; 1: also x element by element).
+template <class T, int RT, int MT, int PIECES, int ALIGN>
+__global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_group) {
     typedef typename T::elem E;
-    const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, m = blockIdx.y;
-    if (n >= a.N) return;
-    const E *x = (const E *)a.x + m * a.x_stride, *s = (const E *)a.scales + (int64_t)n * a.groups;
-    const uint8_t *w = a.w + (int64_t)n * (a.K / 2), *z = a.zeros ? a.zeros + (int64_t)n * a.groups : nullptr;
-    float t = 0;
-    for (int i = lane; i < a.K / 2; i += 64) {
-        const int g = 2 * i / a.group, v = w[i];
-        const int even = z ? (v & 15) - z[g] : ((v & 15) ^ 8) - 8, odd = z ? (v >> 4) - z[g] : ((v >> 4) ^ 8) - 8;
-        t += ((float)x[2 * i] * (float)even + (float)x[2 * i + 1] * (float)odd) * (float)s[g];
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, r = lane & 15, c = lane >> 4;
+    const int n0 = blockIdx.x * (16 * RT), m0 = blockIdx.y * (16 * MT);
+    float *own = (float *)lds + wave * (RT * PIECES * 16 * 2);     // the wave's scales [tile][piece][2][16 outputs]
+    const uint32_t flip = Nibbles<T>::base ^ (a.zeros ? 0u : Nibbles<T>::sign);
+    const typename T::v8 ones = __builtin_bit_cast(typename T::v8, v4u{Nibbles<T>::one, Nibbles<T>::one, Nibbles<T>::one, Nibbles<T>::one});
+
+    // this lane's rows of w, scales and zero points, one for each tile, and its rows of x (past the last one: the last one again)
+    const uint8_t *w[RT], *z[RT];
+    const E *s[RT], *x[MT];
+    for (int t = 0; t < RT; ++t) {
+        const int64_t n = min(n0 + 16 * t + r, a.N - 1);
+        w[t] = a.w + n * (a.K >> 1);
+        s[t] = (const E *)a.scales + n * a.groups;
+        z[t] = a.zeros ? a.zeros + n * a.groups : nullptr;
     }
-    for (int d = 32; d > 0; d >>= 1) t += __shfl_xor(t, d);
-    if (lane == 0) ((E *)a.y)[m * a.y_stride + n] = (E)(t + (a.bias ? (float)((const E *)a.bias)[n] : 0.f));
+    for (int i = 0; i < MT; ++i) x[i] = (const E *)a.x + (int64_t)min(m0 + 16 * i + r, a.M - 1) * a.x_stride;
+
+    struct Stage {
+        v4u w[RT], x[MT][4];
+        E s[RT];
+        uint8_t z[RT];
+    };
+    auto load = [&](int k0, Stage &g) {
+        const int kw = k0 + 32 * c;                                 // the 32 weights this lane reads
+        const int group = (int)fdiv((uint32_t)min(kw, a.K - 1), by_group);
+        for (int t = 0; t < RT; ++t) {
+            if constexpr (ALIGN == 16) {
+                g.w[t] = kw < a.K ? *(const v4u *)(w[t] + (kw >> 1)) : v4u{0, 0, 0, 0};
+            } else if constexpr (ALIGN == 4) {
+                for (int j = 0; j < 4; ++j) g.w[t][j] = kw + 8 * j < a.K ? *(const uint32_t *)(w[t] + ((kw + 8 * j) >> 1)) : 0u;
+            } else {
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t d = 0;
+                    for (int i = 0; i < 4; ++i) d |= (kw + 8 * j + 2 * i < a.K ? (uint32_t)w[t][(kw + 8 * j + 2 * i) >> 1] : 0u) << (8 * i);
+                    g.w[t][j] = d;
+                }
+            }
+            g.s[t] = s[t][group];
+            g.z[t] = z[t] ? z[t][group] : 8;
+        }
+        for (int i = 0; i < MT; ++i)
+            for (int j = 0; j < 4; ++j) {
+                const int k = k0 + 32 * j + 8 * c;
+                if constexpr (ALIGN > 1) {
+                    g.x[i][j] = k < a.K ? *(const v4u *)(x[i] + k) : v4u{0, 0, 0, 0};
+                } else {
+                    for (int e = 0; e < 4; ++e) {
+                        const uint16_t *p = (const uint16_t *)x[i] + k + 2 * e;
+                        g.x[i][j][e] = k + 2 * e < a.K ? p[0] | (uint32_t)p[1] << 16 : 0u;      // (K is even)
+                    }
+                }
+            }
+    };
+
+    v4f acc[RT][MT];
+    for (int t = 0; t < RT; ++t)
+        for (int i = 0; i < MT; ++i) acc[t][i] = v4f{0, 0, 0, 0};
+
+    const int steps = (a.K + 127) >> 7;
+    Stage now;
+    if (wave < steps) load(wave << 7, now);
+    for (int step = wave; step < steps; step += waves) {
+        Stage next;
+        if (step + waves < steps) load((step + waves) << 7, next);
+        // scales from a lane per output to a lane per four outputs (the accumulators' rows), through the wave's own LDS
+        for (int t = 0; t < RT; ++t) {
+            const int p = PIECES == 4 ? c : PIECES == 2 ? c >> 1 : 0;
+            const float sc = (float)now.s[t];
+            own[((t * PIECES + p) * 2 + 0) * 16 + r] = sc;
+            own[((t * PIECES + p) * 2 + 1) * 16 + r] = sc * (float)(16 + now.z[t]);
+            exchange_quarters(now.w[t]);
+        }
+        typename T::v8 xv[MT][4];
+        float sum[MT][PIECES];                                      // (every row of the product with ones is the same)
+        for (int i = 0; i < MT; ++i)
+            for (int p = 0; p < PIECES; ++p) {
+                v4f t{0, 0, 0, 0};
+                for (int j = p * 4 / PIECES; j < (p + 1) * 4 / PIECES; ++j) {
+                    xv[i][j] = ordered<T>(now.x[i][j]);
+                    t = T::mfma16(ones, xv[i][j], t);
+                }
+                sum[i][p] = t[0];
+            }
+        __builtin_amdgcn_wave_barrier();
+        for (int t = 0; t < RT; ++t)
+            for (int p = 0; p < PIECES; ++p) {
+                v4f part[MT];
+                for (int i = 0; i < MT; ++i) part[i] = v4f{0, 0, 0, 0};
+                for (int j = p * 4 / PIECES; j < (p + 1) * 4 / PIECES; ++j) {
+                    const typename T::v8 wv = expand<T>(now.w[t][j], flip);
+                    for (int i = 0; i < MT; ++i) part[i] = T::mfma16(wv, xv[i][j], part[i]);
+                }
+                const v4f sc = *(const v4f *)(own + ((t * PIECES + p) * 2 + 0) * 16 + 4 * c), sz = *(const v4f *)(own + ((t * PIECES + p) * 2 + 1) * 16 + 4 * c);
+                for (int i = 0; i < MT; ++i)
+                    for (int e = 0; e < 4; ++e) acc[t][i][e] = fmaf(sc[e], part[i][e], fmaf(-sz[e], sum[i][p], acc[t][i][e]));
+            }
+        __builtin_amdgcn_wave_barrier();
+        now = next;
+    }
+
+    // the waves' parts of 16 rows of y at a time: [wave][row][16 RT outputs, four more to spread the rows over the banks]
+    constexpr int kRow = 16 * RT + 4;
+    float *red = (float *)lds;
+    E *y = (E *)a.y;
+    for (int i = 0; i < MT; ++i) {
+        __syncthreads();
+        for (int t = 0; t < RT; ++t) *(v4f *)(red + (wave * 16 + r) * kRow + 16 * t + 4 * c) = acc[t][i];
+        __syncthreads();
+        for (int e = threadIdx.x; e < 256 * RT; e += blockDim.x) {
+            const int m = e / (16 * RT), n = e % (16 * RT);
+            float v = 0;
+            for (int k = 0; k < waves; ++k) v += red[(k * 16 + m) * kRow + n];
+            if (m0 + 16 * i + m < a.M && n0 + n < a.N) {
+                if (a.bias) v += (float)((const E *)a.bias)[n0 + n];
+                y[(int64_t)(m0 + 16 * i + m) * a.y_stride + n0 + n] = (E)v;
+            }
+        }
+    }
+}
+
+template <class T, int RT, int MT, int PIECES, int ALIGN>
+hawq_status launch(const LinearW4Args &a, hipStream_t s) {
+    const int steps = (a.K + 127) / 128, waves = steps < 8 ? steps : 8;
+    const size_t scales = (size_t)waves * RT * PIECES * 16 * 2 * 4, sums = (size_t)waves * 16 * (16 * RT + 4) * 4;
+    const dim3 grid((unsigned)((a.N + 16 * RT - 1) / (16 * RT)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
+    if (grid.y > 65535) return HAWQ_ERR_UNSUPPORTED;
+    linear_w4<T, RT, MT, PIECES, ALIGN><<<grid, 64 * waves, scales > sums ? scales : sums, s>>>(a, fast_div((uint32_t)a.group));
+    return check_launch();
+}
+
+template <class T, int PIECES, int ALIGN>
+hawq_status pick_tiles(const LinearW4Args &a, hipStream_t s) {
+    if constexpr (ALIGN == 16) {
+        if (a.N >= 64 * 192) return a.M <= 16 ? launch<T, 4, 1, PIECES, ALIGN>(a, s) : a.M <= 32 ? launch<T, 4, 2, PIECES, ALIGN>(a, s) : launch<T, 2, 4, PIECES, ALIGN>(a, s);
+        if (a.N >= 32 * 192) return a.M <= 16 ? launch<T, 2, 1, PIECES, ALIGN>(a, s) : a.M <= 32 ? launch<T, 2, 2, PIECES, ALIGN>(a, s) : launch<T, 2, 4, PIECES, ALIGN>(a, s);
+    }
+    return a.M <= 16 ? launch<T, 1, 1, PIECES, ALIGN>(a, s) : launch<T, 1, 4, PIECES, ALIGN>(a, s);
+}
+
+template <class T, int ALIGN>
+hawq_status pick_pieces(const LinearW4Args &a, hipStream_t s) {
+    return a.group % 128 == 0 ? pick_tiles<T, 1, ALIGN>(a, s) : a.group % 64 == 0 ? pick_tiles<T, 2, ALIGN>(a, s) : pick_tiles<T, 4, ALIGN>(a, s);
+}
+
+template <class T>
+hawq_status pick_align(const LinearW4Args &a, hipStream_t s) {
+    const bool x16 = ((uintptr_t)a.x & 15) == 0 && a.x_stride % 8 == 0;
+    if (x16 && a.K % 32 == 0 && ((uintptr_t)a.w & 15) == 0) return pick_pieces<T, 16>(a, s);
+    if (x16 && a.K % 8 == 0 && ((uintptr_t)a.w & 3) == 0) return pick_pieces<T, 4>(a, s);
+    return pick_pieces<T, 1>(a, s);
 }
 
 }  // namespace
 
-hawq_status launch_linear_w4(const LinearW4Args &a, hipStream_t s) {
-    if (a.M > 65535) return HAWQ_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((a.N + 3) / 4), (unsigned)a.M);
-    if (a.dtype == HAWQ_F16) linear_w4_any<F16><<<grid, 256, 0, s>>>(a);
-    else linear_w4_any<BF16><<<grid, 256, 0, s>>>(a);
-    return check_launch();
-}
+hawq_status launch_linear_w4(const LinearW4Args &a, hipStream_t s) { return a.dtype == HAWQ_F16 ? pick_align<F16>(a, s) : pick_align<BF16>(a, s); }
 
 }  // namespace hawq

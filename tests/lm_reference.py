@@ -77,7 +77,7 @@ def codes(rows):
     rows = rows.astype(np.float32)
     good = np.isfinite(rows).all(axis=-1)
     with np.errstate(invalid="ignore", divide="ignore"):
-        scale = (np.abs(rows).max(axis=-1) / np.float32(127)).astype(np.float32)
+        scale = (np.abs(rows).max(axis=-1) * (np.float32(1) / np.float32(127))).astype(np.float32)
         q = np.rint(rows / scale[..., None]).astype(np.float32)
     scale = np.where(good, scale, np.float32("nan"))
     q = np.where((scale > 0)[..., None], np.clip(q, -127, 127), 0)
