@@ -29,8 +29,9 @@ __global__ __launch_bounds__(64) void attn_tree_any(AttnTreeArgs a) {
         const int64_t f = (p * a.cache.page + at) * a.kv_heads + hk;
         return {(const char *)a.cache.k + e * size, (const char *)a.cache.v + e * size, codes ? a.cache.ks[f] : 1.f, codes ? a.cache.vs[f] : 1.f, codes};
     };
-    attend_row<T>((const E *)a.q + row * a.q_token + h * a.q_head, (E *)a.y + row * a.y_token + h * a.y_head, a.head_dim, a.scale, cached + drafts, q_lds, key,
-                  [&](int j) { return j < cached ? (uint32_t)table[fdiv((uint32_t)j, a.cache.by_page)] < (uint32_t)a.cache.n_pages : (seen >> (j - cached) & 1) != 0; });
+    const auto visible = [&](int j) { return j < cached ? (uint32_t)table[fdiv((uint32_t)j, a.cache.by_page)] < (uint32_t)a.cache.n_pages : (seen >> (j - cached) & 1) != 0; };
+    store_row<T>(attend_row<T>((const E *)a.q + row * a.q_token + h * a.q_head, a.head_dim, a.scale, 0, cached + drafts, q_lds, key, visible),
+                 (E *)a.y + row * a.y_token + h * a.y_head, a.head_dim);
 }
 
 }  // namespace

@@ -90,6 +90,13 @@ hawq_status launch_attn_tree(const AttnTreeArgs &a, hipStream_t s);
 hawq_status launch_cache_plan(const CachePlanArgs &a, hipStream_t s);
 hawq_status launch_cache_store(const CacheStoreArgs &a, hipStream_t s);
 
+// Buffer of `bytes` bytes at p, both the same in every lane: made of scalars where the compiler does not see that they are.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t scalar_rsrc(const void *p, uint32_t bytes) {
+    const uint64_t at = (uint64_t)p;
+    const uint64_t s = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32;
+    return __builtin_amdgcn_make_buffer_rsrc((void *)s, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
 // Rows [from, to) of sequence b, whatever the starts hold: inside [0, total) and not negative in number.
 __device__ __forceinline__ void sequence_rows(const int32_t *starts, int b, int total, int &from, int &to) {
     from = min(max(starts[b], 0), total);
