@@ -1,49 +1,514 @@
 // Attention of drafted tokens over a paged cache and over one another.
+//
+// Matrix-core kernel.  The rows that share a key head (drafts x heads of the group) are taken 16, 32 or 64 to a workgroup, whose
+// waves walk over the cache 32 keys at a time, each wave every W-th of these chunks, and join their running maxima, sums and
+// outputs in LDS at the end; a long cache is shared out to several workgroups, whose parts a second launch joins.  As in prompt
+// attention the scores are computed transposed, S^T = K Q^T and O^T = V^T P^T: K's operand is read from memory straight into
+// registers, P's is the accumulator of S^T as it is, V comes through the wave's own LDS and its transposing read.  Keys are
+// looked up in the block table one chunk ahead of their loads, and loaded one chunk ahead of their use.
+//
+// An 8-bit cache's codes become 16-bit floats exactly; a key's scale multiplies its score.  A value's scale would drive f16
+// weights below their range, so its logarithm joins the exponent instead: the stored weight is exp2(s + log2 vs - m) with the
+// maximum m taken of that sum, and the sum of weights adds it divided by vs.
+//
+// Bound by the cache's bytes.  Rows whose result is NaN are computed again by the plain path: 0 times an unseen infinity.
 #include "attn_any.h"
 
 namespace hawq {
 
 namespace {
 
+constexpr float kLog2e = 1.4426950408889634f;
+
+// One request and head of keys as a sequence of positions: cached tokens, then from position `pad` on the drafts.
 template <class T>
-__global__ __launch_bounds__(64) void attn_tree_any(AttnTreeArgs a) {
+struct TreeKeys {
     typedef typename T::elem E;
-    __shared__ float q_lds[256];
-    const int b = blockIdx.z, h = blockIdx.y, hk = h / (a.q_heads / a.kv_heads);
-    int from, to;
-    sequence_rows(a.starts, b, a.total, from, to);
-    const int drafts = min(to - from, a.max_drafts), t = blockIdx.x;
-    if (t >= drafts) return;
-    const int row = from + t, cached = min(max(a.cached[b], 0), a.max_cached);
-    const uint64_t seen = a.mask ? a.mask[row] : t == 63 ? ~0ull : (2ull << t) - 1;
-    const int32_t *table = a.table + (int64_t)b * a.table_stride;
-    const bool codes = a.cache.dtype == HAWQ_S8;
-    const int size = codes ? 1 : 2;
-    auto key = [&](int j) -> KeyRow {
-        if (j >= cached) {
-            const int64_t r = from + j - cached;
+    const AttnTreeArgs &a;
+    int hk, from, drafts, cached, pad;
+    const int32_t *table;
+
+    __device__ __forceinline__ TreeKeys(const AttnTreeArgs &args, int b, int head, int first) : a(args), hk(head), from(first) {
+        int to;
+        sequence_rows(a.starts, b, a.total, from, to);
+        drafts = min(to - from, a.max_drafts);
+        cached = min(max(a.cached[b], 0), a.max_cached);
+        pad = cached;
+        table = a.table + (int64_t)b * a.table_stride;
+    }
+    __device__ __forceinline__ bool on_a_page(int j) const { return (uint32_t)table[fdiv((uint32_t)j, a.cache.by_page)] < (uint32_t)a.cache.n_pages; }
+    __device__ __forceinline__ uint64_t mask(int t) const { return a.mask ? a.mask[from + t] : t == 63 ? ~0ull : (2ull << t) - 1; }
+    __device__ __forceinline__ KeyRow operator()(int j) const {
+        if (j >= pad) {
+            const int64_t r = from + j - pad;
             return {(const E *)a.k + r * a.k_token + hk * a.k_head, (const E *)a.v + r * a.v_token + hk * a.v_head, 1.f, 1.f, false};
         }
-        const int i = (int)fdiv((uint32_t)j, a.cache.by_page), at = j - i * a.cache.page;
+        const bool codes = a.cache.dtype == HAWQ_S8;
+        const int i = (int)fdiv((uint32_t)j, a.cache.by_page), at = j - i * a.cache.page, size = codes ? 1 : 2;
         const int64_t p = table[i], e = p * a.cache.page_stride + at * a.cache.token_stride + hk * a.cache.head_stride;
         const int64_t f = (p * a.cache.page + at) * a.kv_heads + hk;
         return {(const char *)a.cache.k + e * size, (const char *)a.cache.v + e * size, codes ? a.cache.ks[f] : 1.f, codes ? a.cache.vs[f] : 1.f, codes};
+    }
+    __device__ __forceinline__ bool visible(int j, uint64_t seen) const {
+        return j < pad ? j < cached && on_a_page(j) : j - pad < drafts && (seen >> (j - pad) & 1) != 0;
+    }
+    __device__ __forceinline__ RowSums attend(int t, int h, int begin, int end, float *q_lds) const {
+        const uint64_t seen = mask(t);
+        return attend_row<T>((const E *)a.q + (int64_t)(from + t) * a.q_token + h * a.q_head, a.head_dim, a.scale, begin, end, q_lds, *this,
+                             [&](int j) { return visible(j, seen); });
+    }
+    __device__ __forceinline__ E *out(int t, int h) const { return (E *)a.y + (int64_t)(from + t) * a.y_token + h * a.y_head; }
+};
+
+// any head dimension, stride and alignment: a wave per row
+template <class T>
+__global__ __launch_bounds__(64) void attn_tree_any(AttnTreeArgs a) {
+    __shared__ float q_lds[256];
+    const int t = blockIdx.x, h = blockIdx.y;
+    const TreeKeys<T> keys(a, blockIdx.z, h / (a.q_heads / a.kv_heads), 0);
+    if (t >= keys.drafts) return;
+    store_row<T>(keys.attend(t, h, 0, keys.cached + keys.drafts, q_lds), keys.out(t, h), a.head_dim);
+}
+
+struct TreePlan {
+    int32_t rows;              // rows of a workgroup: 16, 32, 64
+    int32_t row_tiles;         // workgroups over a request's rows
+    int32_t chunks, splits;    // chunks of 32 keys of a workgroup, workgroups over a request's chunks at most
+    FastDiv by_group;          // heads of a group
+};
+
+constexpr int kChunk = 32;
+
+int waves_of(int rows) { return rows == 64 ? 4 : 8; }
+
+TreePlan tree_plan(const AttnTreeArgs &a) {
+    TreePlan p;
+    const int group = a.q_heads / a.kv_heads;
+    const int64_t rows = (int64_t)a.max_drafts * group;
+    p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    p.row_tiles = (int32_t)((rows + p.rows - 1) / p.rows);
+    p.by_group = fast_div((uint32_t)group);
+    const int waves = waves_of(p.rows);
+    const int64_t most = (a.max_cached + kChunk - 1) / kChunk + (a.max_drafts + kChunk - 1) / kChunk, one = (int64_t)a.n_seqs * a.kv_heads * p.row_tiles;
+    // enough workgroups for every compute unit some times over (requests are of unequal length), but at least four chunks for a wave
+    int64_t chunks = (most * one + 2047) / 2048;
+    chunks = (chunks + waves - 1) / waves * waves;
+    p.chunks = (int32_t)(chunks < 4 * waves ? 4 * waves : chunks);
+    p.splits = (int32_t)((most + p.chunks - 1) / p.chunks);
+    return p;
+}
+
+// partial sums: [row][q head][split][head_dim] floats, then [row][q head][split][2]: maximum (powers of two) and sum of weights
+__device__ __forceinline__ int64_t part_of(const AttnTreeArgs &a, const TreePlan &p, int64_t row, int h, int split) { return (row * a.q_heads + h) * p.splits + split; }
+__device__ __forceinline__ float *stats_of(const AttnTreeArgs &a, const TreePlan &p) { return a.partial + (int64_t)a.total * a.q_heads * p.splits * a.head_dim; }
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+
+// eight codes as T, exactly
+template <class T>
+__device__ __forceinline__ typename T::v8 from_codes(uint32_t lo, uint32_t hi) {
+    typename T::v8 r;
+    asm("" : "+v"(lo), "+v"(hi));        // (else the bytes are split where they are loaded, a register each)
+    for (int i = 0; i < 4; ++i) {
+        r[i] = (typename T::elem)(float)(int8_t)(lo >> (8 * i));
+        r[4 + i] = (typename T::elem)(float)(int8_t)(hi >> (8 * i));
+    }
+    return r;
+}
+
+__device__ __forceinline__ float max_of_quarters(float v) {
+    v2u x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
+    x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
+}
+__device__ __forceinline__ float sum_of_quarters(float v) {
+    v2u x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x.x) + __uint_as_float(x.y);
+    x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(x.x) + __uint_as_float(x.y);
+}
+__device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__shfl((int)v, lane) | (uint64_t)(uint32_t)__shfl((int)(v >> 32), lane) << 32);
+}
+
+// CODES: 8-bit cache.  DT: 32-element parts of the head dimension (2, 3, 4; with codes 2, 4).  NT: 16-row tiles.
+template <class T, bool CODES, int DT, int NT>
+__global__ __launch_bounds__(NT == 4 ? 256 : 512, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArgs a, TreePlan p, float by_log2e, uint32_t negate) {
+    typedef typename T::elem E;
+    constexpr int W = NT == 4 ? 4 : 8, PITCH = DT == 2 ? 128 : 256, D16 = 2 * DT, DP = 32 * DT, TILE = kChunk * PITCH, V_LOADS = TILE / 1024;
+    constexpr int RED = 16 * (DP + 4) * 4 > TILE ? 16 * (DP + 4) * 4 : TILE;       // a wave's part of 16 rows, when the waves join
+    __shared__ __align__(1024) char v_even[W * RED], v_odd[W * TILE];
+    __shared__ float scales[W][2][kChunk], stat[W][2][16 * NT], joined[2][16 * NT], q_lds[W][256];
+    __shared__ uint32_t bad[2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane >> 4, r = lane & 15;
+    int id = blockIdx.x;
+    const int split = id % p.splits; id /= p.splits;
+    const int hk = id % a.kv_heads; id /= a.kv_heads;
+    const int tile = id % p.row_tiles, b = id / p.row_tiles;
+    TreeKeys<T> keys(a, b, hk, 0);
+    const int group = a.q_heads / a.kv_heads, n_rows = keys.drafts * group, row0 = tile * 16 * NT;
+    const int cached_chunks = (keys.cached + kChunk - 1) / kChunk, n_chunks = cached_chunks + (keys.drafts + kChunk - 1) / kChunk;
+    const int first = split * p.chunks, last = min(n_chunks, first + p.chunks);
+    if (row0 >= n_rows || first >= last) return;
+    keys.pad = cached_chunks * kChunk;
+
+    // queries: operand B; d of lane, step s: 32 s + 8 c, with codes 64 (s / 2) + 16 c + 8 (s % 2) (16 codes are one load)
+    typename T::v8 q[NT][DT];
+    uint64_t mask[NT];
+    for (int n = 0; n < NT; ++n) {
+        const int row = min(row0 + 16 * n + r, n_rows - 1), t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
+        const E *at = (const E *)a.q + (int64_t)(keys.from + t) * a.q_token + h * a.q_head;
+        mask[n] = keys.mask(t);
+        for (int s = 0; s < DT; ++s) {
+            const int d = CODES ? 64 * (s >> 1) + 16 * c + 8 * (s & 1) : 32 * s + 8 * c;
+            v4u x = d < a.head_dim ? *(const v4u *)(at + d) : v4u{0, 0, 0, 0};
+            x ^= negate;
+            q[n][s] = __builtin_bit_cast(typename T::v8, x);
+        }
+    }
+
+    // swizzle of V's rows in LDS: 16-byte piece i of row x lies at piece i ^ f(x)
+    auto f = [](int x) { return PITCH == 256 ? (x & 7) << 1 : (x & 6); };
+    const int v_base = (4 * c + ((lane >> 2) & 3)) * PITCH + ((f(4 * c + ((lane >> 2) & 3)) | ((lane >> 1) & 1)) << 4) + (lane & 1) * 8;
+
+    struct Chunk {
+        v4u k[2][CODES ? DT / 2 : DT], v[CODES ? V_LOADS / 2 : 1];
+        float ks, vs;
+        uint32_t seen;
     };
-    const auto visible = [&](int j) { return j < cached ? (uint32_t)table[fdiv((uint32_t)j, a.cache.by_page)] < (uint32_t)a.cache.n_pages : (seen >> (j - cached) & 1) != 0; };
-    store_row<T>(attend_row<T>((const E *)a.q + row * a.q_token + h * a.q_head, a.head_dim, a.scale, 0, cached + drafts, q_lds, key, visible),
-                 (E *)a.y + row * a.y_token + h * a.y_head, a.head_dim);
+    // where the chunk's keys lie: this lane's key (lane & 31), elements from the cache's start; and whether it has a page
+    auto look_up = [&](int chunk, int64_t &off, int64_t &scale_at, bool &ok) {
+        const int j = chunk * kChunk + (lane & 31), i = min(j, keys.cached - 1);      // (past the last one: the last one, not seen)
+        const int pg = (int)fdiv((uint32_t)i, a.cache.by_page), at = i - pg * a.cache.page, page = keys.table[pg];
+        ok = (uint32_t)page < (uint32_t)a.cache.n_pages;
+        const int64_t good = ok ? page : 0;
+        off = good * a.cache.page_stride + at * a.cache.token_stride + hk * a.cache.head_stride;
+        scale_at = (good * a.cache.page + at) * a.kv_heads + hk;
+        ok &= j < keys.cached;
+    };
+    auto load_cached = [&](int64_t off, int64_t scale_at, bool ok, Chunk &g, char *vt) {
+        g.seen = (uint32_t)__ballot(ok);
+        if constexpr (CODES) {
+            g.ks = a.cache.ks[scale_at];
+            g.vs = a.cache.vs[scale_at];
+        }
+        for (int t = 0; t < 2; ++t) {
+            const int64_t at = shfl64(off, 16 * t + r);
+            for (int s = 0; s < (CODES ? DT / 2 : DT); ++s) {
+                const int d = CODES ? 64 * s + 16 * c : 32 * s + 8 * c;              // (past the head's elements: the first ones, times 0 in q)
+                g.k[t][s] = *(const v4u *)((const char *)a.cache.k + (at + (d < a.head_dim ? d : 0)) * (CODES ? 1 : 2));
+            }
+        }
+        if constexpr (CODES) {
+            constexpr int LANES = PITCH / 32;                                        // lanes of a row of codes
+            const int piece = lane % LANES;
+            for (int i = 0; i < V_LOADS / 2; ++i) {
+                const int64_t at = shfl64(off, i * (64 / LANES) + lane / LANES);
+                g.v[i] = *(const v4u *)((const int8_t *)a.cache.v + at + (piece * 16 < a.head_dim ? piece * 16 : 0));   // (not stored)
+            }
+        } else {
+            constexpr int LANES = PITCH / 16;
+            for (int i = 0; i < V_LOADS; ++i) {
+                const int row = i * (64 / LANES) + lane / LANES, piece = (lane % LANES) ^ f(row);
+                const int64_t at = shfl64(off, row) + (piece * 8 < a.head_dim ? piece * 8 : 0);   // (past the head's elements: any, not stored)
+                __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)((const E *)a.cache.v + at), (__attribute__((address_space(3))) void *)(vt + i * 1024), 16, 0, 0);
+            }
+        }
+    };
+
+    v4f o[NT][D16];
+    float m[NT], total[NT];
+    for (int n = 0; n < NT; ++n) {
+        m[n] = -INFINITY;
+        total[n] = 0;
+        for (int d = 0; d < D16; ++d) o[n][d] = v4f{0, 0, 0, 0};
+    }
+
+    // scores in sc (times c = scale log2 e where WEIGHTED: times the key's own factor too), 32 keys' values in vt
+    auto join = [&](v4f (&sc)[2][NT], auto weighted, const float *vlog, const float *vinv, const char *vt) {
+        constexpr bool WEIGHTED = decltype(weighted)::value;
+        typename T::v8 pv[NT];
+        float lv[2][4], iv[2][4];
+        if constexpr (WEIGHTED)
+            for (int t = 0; t < 2; ++t) {
+                *(v4f *)lv[t] = *(const v4f *)(vlog + 16 * t + 4 * c);
+                *(v4f *)iv[t] = *(const v4f *)(vinv + 16 * t + 4 * c);
+            }
+        for (int n = 0; n < NT; ++n) {
+            float top = -INFINITY;
+            for (int t = 0; t < 2; ++t)
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (WEIGHTED) sc[t][n][e] += lv[t][e];
+                    top = fmaxf(top, sc[t][n][e]);
+                }
+            top = max_of_quarters(top);
+            if (__any(top > m[n] + 8.f)) {       // (as in prompt attention: powers of two up to 2^8 over the maximum do no harm)
+                const float next = fmaxf(m[n], top), keep = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - next);
+                m[n] = next;
+                total[n] *= keep;
+                for (int d = 0; d < D16; ++d) o[n][d] *= keep;
+            }
+            const float off = m[n] == -INFINITY ? 0.f : m[n];
+            for (int t = 0; t < 2; ++t)
+                for (int e = 0; e < 4; ++e) {
+                    const float w = __builtin_amdgcn_exp2f(sc[t][n][e] - off);
+                    if constexpr (WEIGHTED) total[n] = fmaf(w, iv[t][e], total[n]);
+                    else total[n] += w;
+                    pv[n][4 * t + e] = (E)w;
+                }
+        }
+        for (int d = 0; d < D16; ++d) {
+            const char *at = vt + (v_base ^ (d << 5));
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)at);
+            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(at + 16 * PITCH));
+            const v8s both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            for (int n = 0; n < NT; ++n) o[n][d] = T::mfma16(__builtin_bit_cast(typename T::v8, both), pv[n], o[n][d]);
+        }
+    };
+
+    auto use_cached = [&](Chunk &g, char *vt) {
+        float *vlog = scales[wave][0], *vinv = scales[wave][1];
+        float kf[2][4];
+        if constexpr (CODES) {
+            __builtin_amdgcn_wave_barrier();
+            const bool mine = g.seen >> (lane & 31) & 1;                             // (a key that is not seen has no scale)
+            if (lane < kChunk) vlog[lane] = mine ? g.ks * by_log2e : 0.f;
+            __builtin_amdgcn_wave_barrier();
+            for (int t = 0; t < 2; ++t) *(v4f *)kf[t] = *(const v4f *)(vlog + 16 * t + 4 * c);
+            __builtin_amdgcn_wave_barrier();
+            const float v = mine ? fmaxf(g.vs, 0x1p-100f) : 1.f;
+            if (lane < kChunk) {
+                vlog[lane] = mine && g.vs != g.vs ? g.vs : __builtin_amdgcn_logf(v);
+                vinv[lane] = 1.f / v;
+            }
+            // V's codes to LDS as T
+            constexpr int LANES = PITCH / 32;
+            for (int i = 0; i < V_LOADS / 2; ++i) {
+                const int row = i * (64 / LANES) + lane / LANES, piece = lane % LANES * 2;
+                *(typename T::v8 *)(vt + row * PITCH + ((piece ^ f(row)) << 4)) = from_codes<T>(g.v[i].x, g.v[i].y);
+                *(typename T::v8 *)(vt + row * PITCH + (((piece + 1) ^ f(row)) << 4)) = from_codes<T>(g.v[i].z, g.v[i].w);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        v4f sc[2][NT];
+        for (int t = 0; t < 2; ++t) {
+            for (int n = 0; n < NT; ++n) sc[t][n] = v4f{0, 0, 0, 0};
+            for (int s = 0; s < DT; ++s) {
+                typename T::v8 k;
+                if constexpr (CODES) k = (s & 1) ? from_codes<T>(g.k[t][s >> 1].z, g.k[t][s >> 1].w) : from_codes<T>(g.k[t][s >> 1].x, g.k[t][s >> 1].y);
+                else k = __builtin_bit_cast(typename T::v8, g.k[t][s]);
+                for (int n = 0; n < NT; ++n) sc[t][n] = T::mfma16(k, q[n][s], sc[t][n]);
+            }
+            for (int n = 0; n < NT; ++n)
+                for (int e = 0; e < 4; ++e) sc[t][n][e] *= CODES ? kf[t][e] : by_log2e;
+        }
+        if (g.seen != 0xffffffffu)
+            for (int t = 0; t < 2; ++t)
+                for (int e = 0; e < 4; ++e)
+                    if (!(g.seen >> (16 * t + 4 * c + e) & 1))
+                        for (int n = 0; n < NT; ++n) sc[t][n][e] = -INFINITY;
+        join(sc, std::integral_constant<bool, CODES>{}, vlog, vinv, vt);
+    };
+
+    // a chunk of drafts: rows of k and v in T, seen as the masks say
+    auto use_drafts = [&](int chunk, char *vt) {
+        const int j0 = (chunk - cached_chunks) * kChunk;
+        constexpr int LANES = PITCH / 16;
+        for (int i = 0; i < V_LOADS; ++i) {
+            const int row = i * (64 / LANES) + lane / LANES, piece = lane % LANES;
+            const int64_t at = keys.from + min(j0 + row, keys.drafts - 1);
+            const v4u x = *(const v4u *)((const E *)a.v + at * a.v_token + hk * a.v_head + (piece * 8 < a.head_dim ? piece * 8 : 0));
+            *(v4u *)(vt + row * PITCH + ((piece ^ f(row)) << 4)) = x;
+        }
+        __builtin_amdgcn_wave_barrier();
+        v4f sc[2][NT];
+        for (int t = 0; t < 2; ++t) {
+            for (int n = 0; n < NT; ++n) sc[t][n] = v4f{0, 0, 0, 0};
+            const E *at = (const E *)a.k + (int64_t)(keys.from + min(j0 + 16 * t + r, keys.drafts - 1)) * a.k_token + hk * a.k_head;
+            for (int s = 0; s < DT; ++s) {
+                const int d = CODES ? 64 * (s >> 1) + 16 * c + 8 * (s & 1) : 32 * s + 8 * c;
+                const v4u k = *(const v4u *)(at + (d < a.head_dim ? d : 0));
+                for (int n = 0; n < NT; ++n) sc[t][n] = T::mfma16(__builtin_bit_cast(typename T::v8, k), q[n][s], sc[t][n]);
+            }
+            for (int n = 0; n < NT; ++n)
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j0 + 16 * t + 4 * c + e;
+                    sc[t][n][e] = j < keys.drafts && (mask[n] >> j & 1) ? sc[t][n][e] * by_log2e : -INFINITY;
+                }
+        }
+        join(sc, std::false_type{}, nullptr, nullptr, vt);
+    };
+
+    {
+        char *ve = v_even + wave * RED, *vo = v_odd + wave * TILE;
+        const int end = min(last, cached_chunks);
+        int chunk = first + wave;
+        int64_t off = 0, scale_at = 0;
+        bool ok = false;
+        Chunk even, odd;
+        if (chunk < end) {
+            look_up(chunk, off, scale_at, ok);
+            load_cached(off, scale_at, ok, even, ve);
+            if (chunk + W < end) look_up(chunk + W, off, scale_at, ok);
+        }
+        while (chunk < end) {
+            // (all loads of this chunk have landed; what is issued next is the following chunk's)
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (chunk + W < end) {
+                load_cached(off, scale_at, ok, odd, vo);
+                if (chunk + 2 * W < end) look_up(chunk + 2 * W, off, scale_at, ok);
+            }
+            use_cached(even, ve);
+            chunk += W;
+            if (chunk >= end) break;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (chunk + W < end) {
+                load_cached(off, scale_at, ok, even, ve);
+                if (chunk + 2 * W < end) look_up(chunk + 2 * W, off, scale_at, ok);
+            }
+            use_cached(odd, vo);
+            chunk += W;
+        }
+        for (; chunk < last; chunk += W) use_drafts(chunk, ve);
+    }
+
+    // the waves join: each row's maximum and sum, then 16 rows' outputs at a time
+    for (int n = 0; n < NT; ++n) {
+        total[n] = sum_of_quarters(total[n]);
+        if (c == 0) {
+            stat[wave][0][16 * n + r] = m[n];
+            stat[wave][1][16 * n + r] = total[n];
+        }
+    }
+    if (threadIdx.x < 2) bad[threadIdx.x] = 0;
+    __syncthreads();
+    if (threadIdx.x < 16 * NT) {
+        float top = -INFINITY, sum = 0;
+        for (int w = 0; w < W; ++w) top = fmaxf(top, stat[w][0][threadIdx.x]);
+        for (int w = 0; w < W; ++w) {
+            const float mw = stat[w][0][threadIdx.x];
+            sum += mw == top ? stat[w][1][threadIdx.x] : stat[w][1][threadIdx.x] * __builtin_amdgcn_exp2f(mw - top);
+        }
+        joined[0][threadIdx.x] = top;
+        joined[1][threadIdx.x] = sum;
+    }
+    __syncthreads();
+    const bool whole = n_chunks <= p.chunks;
+    float *red = (float *)v_even;
+    constexpr int ROW = DP + 4;
+    for (int n = 0; n < NT; ++n) {
+        const float top = joined[0][16 * n + r], keep = m[n] == top ? 1.f : __builtin_amdgcn_exp2f(m[n] - top);
+        for (int d = 0; d < D16; ++d) *(v4f *)(red + wave * (RED / 4) + r * ROW + 16 * d + 4 * c) = o[n][d] * keep;
+        __syncthreads();
+        for (int e = threadIdx.x; e < 16 * DP; e += 64 * W) {
+            const int row = row0 + 16 * n + e / DP, d = e % DP;
+            if (row >= n_rows || d >= a.head_dim) continue;
+            float v = 0;
+            for (int w = 0; w < W; ++w) v += red[w * (RED / 4) + e / DP * ROW + d];
+            const float sum = joined[1][16 * n + e / DP];
+            const int t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
+            if (v != v || sum != sum) atomicOr(&bad[n >> 1], 1u << (16 * (n & 1) + e / DP));
+            if (whole) {
+                keys.out(t, h)[d] = (E)(sum == 0.f ? 0.f : v / sum);
+            } else {
+                const int64_t i = part_of(a, p, keys.from + t, h, split);
+                a.partial[i * a.head_dim + d] = v;
+                if (d < 2) stats_of(a, p)[2 * i + d] = d ? sum : joined[0][16 * n + e / DP];
+            }
+        }
+        __syncthreads();
+    }
+    // rows with a NaN once more, the plain way
+    int nth = 0;
+    for (int half = 0; half < 2; ++half)
+        for (uint32_t left = bad[half]; left; left &= left - 1, ++nth) {
+            if (nth % W != wave) continue;
+            const int row = row0 + 32 * half + __builtin_ctz(left), t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
+            const RowSums s = keys.attend(t, h, first * kChunk, last * kChunk, q_lds[wave]);
+            if (whole) {
+                store_row<T>(s, keys.out(t, h), a.head_dim);
+            } else {
+                const int64_t i = part_of(a, p, keys.from + t, h, split);
+                for (int k = 0; k < 4; ++k)
+                    if (lane + 64 * k < a.head_dim) a.partial[i * a.head_dim + lane + 64 * k] = s.total == 0.f ? 0.f : s.o[k];
+                if (lane < 2) stats_of(a, p)[2 * i + lane] = lane ? s.total : s.m * kLog2e;
+            }
+        }
+}
+
+// one wave per row: the parts of a request that was shared out
+template <class T>
+__global__ __launch_bounds__(256) void attn_tree_join(AttnTreeArgs a, TreePlan p) {
+    typedef typename T::elem E;
+    const int lane = threadIdx.x & 63, h = blockIdx.x * 4 + (threadIdx.x >> 6), t = blockIdx.y, b = blockIdx.z;
+    if (h >= a.q_heads) return;
+    const TreeKeys<T> keys(a, b, 0, 0);
+    const int n_chunks = (keys.cached + kChunk - 1) / kChunk + (keys.drafts + kChunk - 1) / kChunk;
+    if (t >= keys.drafts || n_chunks <= p.chunks) return;
+    const int n = (n_chunks + p.chunks - 1) / p.chunks;
+    const int64_t first = part_of(a, p, keys.from + t, h, 0);
+    const float *stats = stats_of(a, p) + 2 * first, *part = a.partial + first * a.head_dim;
+    float top = -INFINITY, sum = 0;
+    for (int s = lane; s < n; s += 64) top = fmaxf(top, stats[2 * s]);
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    for (int s = lane; s < n; s += 64) sum += stats[2 * s] == top ? stats[2 * s + 1] : stats[2 * s + 1] * __builtin_amdgcn_exp2f(stats[2 * s] - top);
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    float o[2] = {0, 0};
+    for (int s = 0; s < n; ++s) {
+        const float w = stats[2 * s] == top ? 1.f : __builtin_amdgcn_exp2f(stats[2 * s] - top);
+        for (int k = 0; k < 2; ++k)
+            if (lane + 64 * k < a.head_dim) o[k] += w * part[(int64_t)s * a.head_dim + lane + 64 * k];
+    }
+    E *y = keys.out(t, h);
+    for (int k = 0; k < 2; ++k)
+        if (lane + 64 * k < a.head_dim) y[lane + 64 * k] = (E)(sum == 0.f ? 0.f : o[k] / sum);
+}
+
+// Rows read in whole vectors.  (Pointers are 0 where only the workspace is asked for.)
+bool matrix_form(const AttnTreeArgs &a) {
+    const bool codes = a.cache.dtype == HAWQ_S8;
+    const int64_t rows = a.q_token | a.q_head | a.k_token | a.k_head | a.v_token | a.v_head, cache = a.cache.page_stride | a.cache.token_stride | a.cache.head_stride;
+    return a.head_dim <= 128 && a.head_dim % (codes ? 16 : 8) == 0 && rows % 8 == 0 && cache % (codes ? 16 : 8) == 0 &&
+           (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.cache.k | (uintptr_t)a.cache.v) & 15) == 0;
+}
+
+template <class T, bool CODES, int DT>
+void launch_rows(const AttnTreeArgs &a, const TreePlan &p, unsigned blocks, hipStream_t s) {
+    const float c = fmaxf(fabsf(a.scale) * kLog2e, 1.2e-38f);       // (a negative scale: -q; zero: as good as the smallest number)
+    const uint32_t negate = a.scale < 0 ? 0x80008000u : 0u;
+    if (p.rows == 16) attn_tree<T, CODES, DT, 1><<<blocks, 512, 0, s>>>(a, p, c, negate);
+    else if (p.rows == 32) attn_tree<T, CODES, DT, 2><<<blocks, 512, 0, s>>>(a, p, c, negate);
+    else attn_tree<T, CODES, DT, 4><<<blocks, 256, 0, s>>>(a, p, c, negate);
+}
+
+template <class T>
+hawq_status launch(const AttnTreeArgs &a, hipStream_t s) {
+    const TreePlan p = tree_plan(a);
+    const int64_t blocks = (int64_t)a.n_seqs * a.kv_heads * p.row_tiles * p.splits;
+    if (a.n_seqs > 65535 || a.q_heads > 65535) return HAWQ_ERR_UNSUPPORTED;
+    if (!matrix_form(a) || blocks > INT32_MAX) {
+        attn_tree_any<T><<<dim3((unsigned)a.max_drafts, (unsigned)a.q_heads, (unsigned)a.n_seqs), 64, 0, s>>>(a);
+        return check_launch();
+    }
+    if (a.cache.dtype == HAWQ_S8) {
+        if (a.head_dim <= 64) launch_rows<T, true, 2>(a, p, (unsigned)blocks, s);
+        else launch_rows<T, true, 4>(a, p, (unsigned)blocks, s);
+    } else if (a.head_dim <= 64) launch_rows<T, false, 2>(a, p, (unsigned)blocks, s);
+    else if (a.head_dim <= 96) launch_rows<T, false, 3>(a, p, (unsigned)blocks, s);
+    else launch_rows<T, false, 4>(a, p, (unsigned)blocks, s);
+    if (p.splits > 1) attn_tree_join<T><<<dim3((unsigned)(a.q_heads + 3) / 4, (unsigned)a.max_drafts, (unsigned)a.n_seqs), 256, 0, s>>>(a, p);
+    return check_launch();
 }
 
 }  // namespace
 
-size_t attn_tree_workspace(const AttnTreeArgs &) { return 0; }
-
-hawq_status launch_attn_tree(const AttnTreeArgs &a, hipStream_t s) {
-    if (a.q_heads > 65535 || a.n_seqs > 65535) return HAWQ_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)a.max_drafts, (unsigned)a.q_heads, (unsigned)a.n_seqs);
-    if (a.dtype == HAWQ_F16) attn_tree_any<F16><<<grid, 64, 0, s>>>(a);
-    else attn_tree_any<BF16><<<grid, 64, 0, s>>>(a);
-    return check_launch();
+size_t attn_tree_workspace(const AttnTreeArgs &a) {
+    const TreePlan p = tree_plan(a);
+    return p.splits > 1 ? (size_t)a.total * a.q_heads * p.splits * (a.head_dim + 2) * sizeof(float) : 0;
 }
+
+hawq_status launch_attn_tree(const AttnTreeArgs &a, hipStream_t s) { return a.dtype == HAWQ_F16 ? launch<F16>(a, s) : launch<BF16>(a, s); }
 
 }  // namespace hawq
