@@ -73,13 +73,12 @@ __global__ __launch_bounds__(64) void attn_tree_any(AttnTreeArgs a) {
 struct TreePlan {
     int32_t rows;              // rows of a workgroup: 16, 32, 64
     int32_t row_tiles;         // workgroups over a request's rows
+    int32_t waves;             // its waves
     int32_t chunks, splits;    // chunks of 32 keys of a workgroup, workgroups over a request's chunks at most
     FastDiv by_group;          // heads of a group
 };
 
 constexpr int kChunk = 32;
-
-int waves_of(int rows) { return rows == 64 ? 4 : 8; }
 
 TreePlan tree_plan(const AttnTreeArgs &a) {
     TreePlan p;
@@ -88,12 +87,18 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
     p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     p.row_tiles = (int32_t)((rows + p.rows - 1) / p.rows);
     p.by_group = fast_div((uint32_t)group);
-    const int waves = waves_of(p.rows);
     const int64_t most = (a.max_cached + kChunk - 1) / kChunk + (a.max_drafts + kChunk - 1) / kChunk, one = (int64_t)a.n_seqs * a.kv_heads * p.row_tiles;
-    // enough workgroups for every compute unit some times over (requests are of unequal length), but at least four chunks for a wave
-    int64_t chunks = (most * one + 2047) / 2048;
-    chunks = (chunks + waves - 1) / waves * waves;
-    p.chunks = (int32_t)(chunks < 4 * waves ? 4 * waves : chunks);
+    // a cache of up to 1024 tokens: one workgroup of eight waves does it without a second launch
+    p.waves = p.rows == 16 && most <= 33 ? 8 : 4;
+    if (p.waves == 8) {
+        p.chunks = (int32_t)most;
+        p.splits = 1;
+        return p;
+    }
+    // enough workgroups for every compute unit some times over (requests are of unequal length), but at least two chunks for a wave
+    int64_t chunks = (most * one + 4095) / 4096;
+    chunks = (chunks + p.waves - 1) / p.waves * p.waves;
+    p.chunks = (int32_t)(chunks < 2 * p.waves ? 2 * p.waves : chunks);
     p.splits = (int32_t)((most + p.chunks - 1) / p.chunks);
     return p;
 }
@@ -133,13 +138,14 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__shfl((int)v, lane) | (uint64_t)(uint32_t)__shfl((int)(v >> 32), lane) << 32);
 }
 
-// CODES: 8-bit cache.  DT: 32-element parts of the head dimension (2, 3, 4; with codes 2, 4).  NT: 16-row tiles.
-template <class T, bool CODES, int DT, int NT>
-__global__ __launch_bounds__(NT == 4 ? 256 : 512, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArgs a, TreePlan p, float by_log2e, uint32_t negate) {
+// CODES: 8-bit cache.  WHOLE: every 16 keys of a chunk lie in one page.  DT: 32-element parts of the head dimension (2, 4).
+// NT: 16-row tiles.  W: waves.
+template <class T, bool CODES, bool WHOLE, int DT, int NT, int W>
+__global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArgs a, TreePlan p, float by_log2e, uint32_t negate) {
     typedef typename T::elem E;
-    constexpr int W = NT == 4 ? 4 : 8, PITCH = DT == 2 ? 128 : 256, D16 = 2 * DT, DP = 32 * DT, TILE = kChunk * PITCH, V_LOADS = TILE / 1024;
+    constexpr int PITCH = DT == 2 ? 128 : 256, D16 = 2 * DT, DP = 32 * DT, TILE = kChunk * PITCH, V_LOADS = TILE / 1024;
     constexpr int RED = 16 * (DP + 4) * 4 > TILE ? 16 * (DP + 4) * 4 : TILE;       // a wave's part of 16 rows, when the waves join
-    __shared__ __align__(1024) char v_even[W * RED], v_odd[W * TILE];
+    __shared__ __align__(1024) char v_even[W * RED], v_odd[CODES ? 16 : W * TILE];   // (codes pass through registers: one buffer)
     __shared__ float scales[W][2][kChunk], stat[W][2][16 * NT], joined[2][16 * NT], q_lds[W][256];
     __shared__ uint32_t bad[2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane >> 4, r = lane & 15;
@@ -178,43 +184,87 @@ __global__ __launch_bounds__(NT == 4 ? 256 : 512, NT == 4 ? 1 : 2) void attn_tre
         float ks, vs;
         uint32_t seen;
     };
-    // where the chunk's keys lie: this lane's key (lane & 31), elements from the cache's start; and whether it has a page
-    auto look_up = [&](int chunk, int64_t &off, int64_t &scale_at, bool &ok) {
-        const int j = chunk * kChunk + (lane & 31), i = min(j, keys.cached - 1);      // (past the last one: the last one, not seen)
-        const int pg = (int)fdiv((uint32_t)i, a.cache.by_page), at = i - pg * a.cache.page, page = keys.table[pg];
-        ok = (uint32_t)page < (uint32_t)a.cache.n_pages;
-        const int64_t good = ok ? page : 0;
-        off = good * a.cache.page_stride + at * a.cache.token_stride + hk * a.cache.head_stride;
-        scale_at = (good * a.cache.page + at) * a.kv_heads + hk;
-        ok &= j < keys.cached;
+    // Where a chunk's keys lie, in elements from the cache's start: this lane's key (lane & 31), or, WHOLE, the two tiles of 16
+    // keys; their scales' places; which keys are seen.  A key past the last one is the last one, not seen.
+    struct Place {
+        int64_t at[2], scale[2];
+        uint32_t seen;
     };
-    auto load_cached = [&](int64_t off, int64_t scale_at, bool ok, Chunk &g, char *vt) {
-        g.seen = (uint32_t)__ballot(ok);
-        if constexpr (CODES) {
-            g.ks = a.cache.ks[scale_at];
-            g.vs = a.cache.vs[scale_at];
-        }
-        for (int t = 0; t < 2; ++t) {
-            const int64_t at = shfl64(off, 16 * t + r);
-            for (int s = 0; s < (CODES ? DT / 2 : DT); ++s) {
-                const int d = CODES ? 64 * s + 16 * c : 32 * s + 8 * c;              // (past the head's elements: the first ones, times 0 in q)
-                g.k[t][s] = *(const v4u *)((const char *)a.cache.k + (at + (d < a.head_dim ? d : 0)) * (CODES ? 1 : 2));
-            }
-        }
-        if constexpr (CODES) {
-            constexpr int LANES = PITCH / 32;                                        // lanes of a row of codes
-            const int piece = lane % LANES;
-            for (int i = 0; i < V_LOADS / 2; ++i) {
-                const int64_t at = shfl64(off, i * (64 / LANES) + lane / LANES);
-                g.v[i] = *(const v4u *)((const int8_t *)a.cache.v + at + (piece * 16 < a.head_dim ? piece * 16 : 0));   // (not stored)
+    const int size = CODES ? 1 : 2;
+    auto look_up = [&](int chunk, Place &g) {
+        if constexpr (WHOLE) {
+            g.seen = 0;
+            for (int t = 0; t < 2; ++t) {
+                const int j = chunk * kChunk + 16 * t, n = min(keys.cached - j, 16), i = max(min(j, keys.cached - 1), 0) & ~15;
+                const int pg = (int)fdiv((uint32_t)i, a.cache.by_page), at = i - pg * a.cache.page, page = keys.table[pg];
+                const bool ok = (uint32_t)page < (uint32_t)a.cache.n_pages;
+                const int64_t good = ok ? page : 0;
+                g.at[t] = good * a.cache.page_stride + at * a.cache.token_stride + hk * a.cache.head_stride;
+                g.scale[t] = (good * a.cache.page + at) * a.kv_heads + hk;
+                if (ok && n > 0) g.seen |= (n == 16 ? 0xffffu : (1u << n) - 1) << (16 * t);
             }
         } else {
-            constexpr int LANES = PITCH / 16;
-            for (int i = 0; i < V_LOADS; ++i) {
-                const int row = i * (64 / LANES) + lane / LANES, piece = (lane % LANES) ^ f(row);
-                const int64_t at = shfl64(off, row) + (piece * 8 < a.head_dim ? piece * 8 : 0);   // (past the head's elements: any, not stored)
-                __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)((const E *)a.cache.v + at), (__attribute__((address_space(3))) void *)(vt + i * 1024), 16, 0, 0);
+            const int j = chunk * kChunk + (lane & 31), i = min(j, keys.cached - 1);
+            const int pg = (int)fdiv((uint32_t)i, a.cache.by_page), at = i - pg * a.cache.page, page = keys.table[pg];
+            const bool ok = (uint32_t)page < (uint32_t)a.cache.n_pages;
+            const int64_t good = ok ? page : 0;
+            g.at[0] = good * a.cache.page_stride + at * a.cache.token_stride + hk * a.cache.head_stride;
+            g.scale[0] = (good * a.cache.page + at) * a.kv_heads + hk;
+            g.seen = (uint32_t)__ballot(ok && j < keys.cached);
+        }
+    };
+    // the lanes' loads: K a key and 16 bytes a lane; V a row's pieces side by side (past the head's elements: the first piece -- K's
+    // meet zeros in q, V's are not stored)
+    constexpr int K_LOADS = CODES ? DT / 2 : DT, LANES = CODES ? PITCH / 32 : PITCH / 16, N_V = CODES ? V_LOADS / 2 : V_LOADS, V_ROWS = 64 / LANES;
+    int k_piece[K_LOADS], v_piece[V_LOADS > 1 && PITCH == 256 && !CODES ? 2 : 1];
+    for (int s = 0; s < K_LOADS; ++s) {
+        const int d = CODES ? 64 * s + 16 * c : 32 * s + 8 * c;
+        k_piece[s] = d < a.head_dim ? d : 0;
+    }
+    for (int i = 0; i < (int)(sizeof(v_piece) / sizeof(int)); ++i) {
+        const int d = CODES ? lane % LANES * 16 : ((lane % LANES) ^ f(i * V_ROWS + lane / LANES)) * 8;
+        v_piece[i] = d < a.head_dim ? d : 0;
+    }
+    auto load_cached = [&](const Place &w, Chunk &g, char *vt) {
+        g.seen = w.seen;
+        // row of a tile -> the row read: the last one seen where the tile is not full
+        auto row_of = [&](int t, int row) {
+            if constexpr (WHOLE) {
+                const uint32_t seen = w.seen >> (16 * t) & 0xffffu;
+                return seen == 0xffffu ? row : min(row, max(31 - __builtin_clz(seen | 1u), 0));
             }
+            return row;
+        };
+        auto base_of = [&](const void *p, int t) {                                    // WHOLE: one address for the tile, the same in every lane
+            const uint64_t at = (uint64_t)p + (uint64_t)(w.at[t] * size);
+            return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at) |
+                                  (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32);
+        };
+        if constexpr (CODES) {
+            const int64_t at = WHOLE ? ((lane & 16) ? w.scale[1] : w.scale[0]) + (int64_t)row_of((lane >> 4) & 1, lane & 15) * a.kv_heads : w.scale[0];
+            g.ks = a.cache.ks[at];
+            g.vs = a.cache.vs[at];
+        }
+        for (int t = 0; t < 2; ++t) {
+            if constexpr (WHOLE) {
+                const char *base = base_of(a.cache.k, t);
+                const int row = row_of(t, r) * (int)a.cache.token_stride;
+                for (int s = 0; s < K_LOADS; ++s) g.k[t][s] = *(const v4u *)(base + (uint32_t)((row + k_piece[s]) * size));
+            } else {
+                const int64_t at = shfl64(w.at[0], 16 * t + r);
+                for (int s = 0; s < K_LOADS; ++s) g.k[t][s] = *(const v4u *)((const char *)a.cache.k + (at + k_piece[s]) * size);
+            }
+        }
+        const char *v_base_of[2] = {WHOLE ? base_of(a.cache.v, 0) : nullptr, WHOLE ? base_of(a.cache.v, 1) : nullptr};
+        for (int i = 0; i < N_V; ++i) {
+            const int row = i * V_ROWS + lane / LANES, piece = v_piece[i % (int)(sizeof(v_piece) / sizeof(int))];
+            const char *at;
+            if constexpr (WHOLE) {
+                const int t = i / (N_V / 2);
+                at = v_base_of[t] + (uint32_t)((row_of(t, row - 16 * t) * (int)a.cache.token_stride + piece) * size);
+            } else at = (const char *)a.cache.v + (shfl64(w.at[0], row) + piece) * size;
+            if constexpr (CODES) g.v[i] = *(const v4u *)at;
+            else __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)at, (__attribute__((address_space(3))) void *)(vt + i * 1024), 16, 0, 0);
         }
     };
 
@@ -342,31 +392,30 @@ __global__ __launch_bounds__(NT == 4 ? 256 : 512, NT == 4 ? 1 : 2) void attn_tre
     };
 
     {
-        char *ve = v_even + wave * RED, *vo = v_odd + wave * TILE;
+        char *ve = v_even + wave * RED, *vo = CODES ? ve : v_odd + wave * TILE;
         const int end = min(last, cached_chunks);
         int chunk = first + wave;
-        int64_t off = 0, scale_at = 0;
-        bool ok = false;
+        Place place;
         Chunk even, odd;
         if (chunk < end) {
-            look_up(chunk, off, scale_at, ok);
-            load_cached(off, scale_at, ok, even, ve);
-            if (chunk + W < end) look_up(chunk + W, off, scale_at, ok);
+            look_up(chunk, place);
+            load_cached(place, even, ve);
+            if (chunk + W < end) look_up(chunk + W, place);
         }
         while (chunk < end) {
             // (all loads of this chunk have landed; what is issued next is the following chunk's)
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             if (chunk + W < end) {
-                load_cached(off, scale_at, ok, odd, vo);
-                if (chunk + 2 * W < end) look_up(chunk + 2 * W, off, scale_at, ok);
+                load_cached(place, odd, vo);
+                if (chunk + 2 * W < end) look_up(chunk + 2 * W, place);
             }
             use_cached(even, ve);
             chunk += W;
             if (chunk >= end) break;
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             if (chunk + W < end) {
-                load_cached(off, scale_at, ok, even, ve);
-                if (chunk + 2 * W < end) look_up(chunk + 2 * W, off, scale_at, ok);
+                load_cached(place, even, ve);
+                if (chunk + 2 * W < end) look_up(chunk + 2 * W, place);
             }
             use_cached(odd, vo);
             chunk += W;
@@ -402,20 +451,23 @@ __global__ __launch_bounds__(NT == 4 ? 256 : 512, NT == 4 ? 1 : 2) void attn_tre
         const float top = joined[0][16 * n + r], keep = m[n] == top ? 1.f : __builtin_amdgcn_exp2f(m[n] - top);
         for (int d = 0; d < D16; ++d) *(v4f *)(red + wave * (RED / 4) + r * ROW + 16 * d + 4 * c) = o[n][d] * keep;
         __syncthreads();
-        for (int e = threadIdx.x; e < 16 * DP; e += 64 * W) {
-            const int row = row0 + 16 * n + e / DP, d = e % DP;
+        for (int e = threadIdx.x; e < 16 * (DP / 4); e += 64 * W) {
+            const int i = e / (DP / 4), d = e % (DP / 4) * 4, row = row0 + 16 * n + i;
             if (row >= n_rows || d >= a.head_dim) continue;
-            float v = 0;
-            for (int w = 0; w < W; ++w) v += red[w * (RED / 4) + e / DP * ROW + d];
-            const float sum = joined[1][16 * n + e / DP];
+            v4f v{0, 0, 0, 0};
+            for (int w = 0; w < W; ++w) v += *(const v4f *)(red + w * (RED / 4) + i * ROW + d);
+            const float sum = joined[1][16 * n + i], any = v.x + v.y + v.z + v.w + sum;
             const int t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
-            if (v != v || sum != sum) atomicOr(&bad[n >> 1], 1u << (16 * (n & 1) + e / DP));
+            if (any != any) atomicOr(&bad[n >> 1], 1u << (16 * (n & 1) + i));
             if (whole) {
-                keys.out(t, h)[d] = (E)(sum == 0.f ? 0.f : v / sum);
+                const float by = 1.f / sum;
+                typename T::v4 y;
+                for (int k = 0; k < 4; ++k) y[k] = (E)(sum == 0.f ? 0.f : v[k] * by);
+                *(typename T::v4 *)(keys.out(t, h) + d) = y;
             } else {
-                const int64_t i = part_of(a, p, keys.from + t, h, split);
-                a.partial[i * a.head_dim + d] = v;
-                if (d < 2) stats_of(a, p)[2 * i + d] = d ? sum : joined[0][16 * n + e / DP];
+                const int64_t at = part_of(a, p, keys.from + t, h, split);
+                *(v4f *)(a.partial + at * a.head_dim + d) = v;
+                if (d == 0) *(float2 *)(stats_of(a, p) + 2 * at) = make_float2(joined[0][16 * n + i], sum);
             }
         }
         __syncthreads();
@@ -451,36 +503,58 @@ __global__ __launch_bounds__(256) void attn_tree_join(AttnTreeArgs a, TreePlan p
     const int64_t first = part_of(a, p, keys.from + t, h, 0);
     const float *stats = stats_of(a, p) + 2 * first, *part = a.partial + first * a.head_dim;
     float top = -INFINITY, sum = 0;
+    float2 o = make_float2(0, 0);
     for (int s = lane; s < n; s += 64) top = fmaxf(top, stats[2 * s]);
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    for (int s = lane; s < n; s += 64) sum += stats[2 * s] == top ? stats[2 * s + 1] : stats[2 * s + 1] * __builtin_amdgcn_exp2f(stats[2 * s] - top);
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    float o[2] = {0, 0};
-    for (int s = 0; s < n; ++s) {
-        const float w = stats[2 * s] == top ? 1.f : __builtin_amdgcn_exp2f(stats[2 * s] - top);
-        for (int k = 0; k < 2; ++k)
-            if (lane + 64 * k < a.head_dim) o[k] += w * part[(int64_t)s * a.head_dim + lane + 64 * k];
+    const int two = min(2 * lane, a.head_dim - 2);      // this lane's elements (past the last: the last ones, not stored)
+    for (int s0 = 0; s0 < n; s0 += 64) {       // 64 parts' weights, a lane each; then their outputs, the loads of eight in flight
+        const int s = s0 + lane;
+        float w = 0;
+        if (s < n) {
+            w = stats[2 * s] == top ? 1.f : __builtin_amdgcn_exp2f(stats[2 * s] - top);
+            sum += w * stats[2 * s + 1];
+        }
+        const int here = min(64, n - s0);
+#pragma unroll 8
+        for (int i = 0; i < here; ++i) {
+            const float wi = __shfl(w, i);
+            const float2 x = *(const float2 *)(part + (int64_t)(s0 + i) * a.head_dim + two);
+            o.x += wi * x.x;
+            o.y += wi * x.y;
+        }
     }
-    E *y = keys.out(t, h);
-    for (int k = 0; k < 2; ++k)
-        if (lane + 64 * k < a.head_dim) y[lane + 64 * k] = (E)(sum == 0.f ? 0.f : o[k] / sum);
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if (2 * lane >= a.head_dim) return;
+    const float by = 1.f / sum;
+    *(typename T::v2 *)(keys.out(t, h) + two) = typename T::v2{(E)(sum == 0.f ? 0.f : o.x * by), (E)(sum == 0.f ? 0.f : o.y * by)};
 }
 
 // Rows read in whole vectors.  (Pointers are 0 where only the workspace is asked for.)
 bool matrix_form(const AttnTreeArgs &a) {
     const bool codes = a.cache.dtype == HAWQ_S8;
     const int64_t rows = a.q_token | a.q_head | a.k_token | a.k_head | a.v_token | a.v_head, cache = a.cache.page_stride | a.cache.token_stride | a.cache.head_stride;
-    return a.head_dim <= 128 && a.head_dim % (codes ? 16 : 8) == 0 && rows % 8 == 0 && cache % (codes ? 16 : 8) == 0 &&
+    return a.head_dim <= 128 && a.head_dim % (codes ? 16 : 8) == 0 && rows % 8 == 0 && (a.y_token | a.y_head) % 4 == 0 && ((uintptr_t)a.y & 7) == 0 && cache % (codes ? 16 : 8) == 0 &&
            (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.cache.k | (uintptr_t)a.cache.v) & 15) == 0;
 }
 
-template <class T, bool CODES, int DT>
+template <class T, bool CODES, bool WHOLE, int DT>
 void launch_rows(const AttnTreeArgs &a, const TreePlan &p, unsigned blocks, hipStream_t s) {
     const float c = fmaxf(fabsf(a.scale) * kLog2e, 1.2e-38f);       // (a negative scale: -q; zero: as good as the smallest number)
     const uint32_t negate = a.scale < 0 ? 0x80008000u : 0u;
-    if (p.rows == 16) attn_tree<T, CODES, DT, 1><<<blocks, 512, 0, s>>>(a, p, c, negate);
-    else if (p.rows == 32) attn_tree<T, CODES, DT, 2><<<blocks, 512, 0, s>>>(a, p, c, negate);
-    else attn_tree<T, CODES, DT, 4><<<blocks, 256, 0, s>>>(a, p, c, negate);
+    if (p.waves == 8) attn_tree<T, CODES, WHOLE, DT, 1, 8><<<blocks, 512, 0, s>>>(a, p, c, negate);
+    else if (p.rows == 16) attn_tree<T, CODES, WHOLE, DT, 1, 4><<<blocks, 256, 0, s>>>(a, p, c, negate);
+    else if (p.rows == 32) attn_tree<T, CODES, WHOLE, DT, 2, 4><<<blocks, 256, 0, s>>>(a, p, c, negate);
+    else attn_tree<T, CODES, WHOLE, DT, 4, 4><<<blocks, 256, 0, s>>>(a, p, c, negate);
+}
+
+template <class T, bool CODES>
+void launch_form(const AttnTreeArgs &a, const TreePlan &p, unsigned blocks, hipStream_t s) {
+    // 16 keys from a multiple of 16 on share a page; their rows lie within 31-bit offsets of the first
+    if (a.cache.page % 16 == 0 && a.cache.token_stride < (1 << 25)) {
+        if (a.head_dim <= 64) launch_rows<T, CODES, true, 2>(a, p, blocks, s);
+        else launch_rows<T, CODES, true, 4>(a, p, blocks, s);
+    } else if (a.head_dim <= 64) launch_rows<T, CODES, false, 2>(a, p, blocks, s);
+    else launch_rows<T, CODES, false, 4>(a, p, blocks, s);
 }
 
 template <class T>
@@ -492,12 +566,8 @@ hawq_status launch(const AttnTreeArgs &a, hipStream_t s) {
         attn_tree_any<T><<<dim3((unsigned)a.max_drafts, (unsigned)a.q_heads, (unsigned)a.n_seqs), 64, 0, s>>>(a);
         return check_launch();
     }
-    if (a.cache.dtype == HAWQ_S8) {
-        if (a.head_dim <= 64) launch_rows<T, true, 2>(a, p, (unsigned)blocks, s);
-        else launch_rows<T, true, 4>(a, p, (unsigned)blocks, s);
-    } else if (a.head_dim <= 64) launch_rows<T, false, 2>(a, p, (unsigned)blocks, s);
-    else if (a.head_dim <= 96) launch_rows<T, false, 3>(a, p, (unsigned)blocks, s);
-    else launch_rows<T, false, 4>(a, p, (unsigned)blocks, s);
+    if (a.cache.dtype == HAWQ_S8) launch_form<T, true>(a, p, (unsigned)blocks, s);
+    else launch_form<T, false>(a, p, (unsigned)blocks, s);
     if (p.splits > 1) attn_tree_join<T><<<dim3((unsigned)(a.q_heads + 3) / 4, (unsigned)a.max_drafts, (unsigned)a.n_seqs), 256, 0, s>>>(a, p);
     return check_launch();
 }

@@ -5,77 +5,181 @@ namespace hawq {
 
 namespace {
 
-__device__ __forceinline__ int wave_scan(int v) {
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d);
-        if ((int)(threadIdx.x & 63) >= d) v += o;
-    }
-    return v;
+constexpr int kThreads = 256, kEach = 8, kPass = kThreads * kEach;    // requests of a thread and of a pass
+constexpr int kSlots = 8;                                             // slots of a thread under way
+
+// ceil(n / page) for n < 2^31
+__device__ __forceinline__ int pages_of(int n, int page, FastDiv by_page) {
+    const int q = (int)fdiv((uint32_t)n, by_page);
+    return q + (q * page < n);
 }
 
-constexpr int kPlanThreads = 256;
+// the last i < n with first[i] <= at (first[0] <= at): requests that get nothing share their neighbour's start and are passed over
+__device__ __forceinline__ int holder(const int *first, int n, int at) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (first[mid] <= at) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
 
-// Every workgroup walks over all requests, kPlanThreads at a time with running totals, and writes of what it meets its own
-// range of slots and (by the request's index) its own share of the table, the starts and the counts.
-__global__ __launch_bounds__(kPlanThreads) void cache_plan(CachePlanArgs a, int slots_per_block) {
-    __shared__ int tokens[kPlanThreads + 1], pages[kPlanThreads], held[kPlanThreads], have[kPlanThreads], wave_sum[2][kPlanThreads / 64];
-    const int tid = threadIdx.x;
+// Every workgroup adds up the tokens and pages of all requests (2048 in a pass: eight of a thread, then across the waves), so that one
+// launch does without an order among workgroups, and writes its own share of the slots and of the pages taken.  A thread finds
+// its first slot's request by bisection and walks on from there.  Bound by the slots' bytes, or by the chain of dependent steps.
+__global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv by_page, int slots_per_block, int pages_per_block) {
+    __shared__ int token[kPass + 1], taken[kPass + 1], held[kPass], wave_sum[2][kThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, last = gridDim.x - 1;
     const int64_t s0 = (int64_t)blockIdx.x * slots_per_block, s1 = min(s0 + slots_per_block, a.n_slots);
-    int token_base = 0, page_base = 0;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += kPlanThreads) {
-        const int b = b0 + tid;
-        const int c = b < a.n_seqs ? max(a.cached[b], 0) : 0, f = b < a.n_seqs ? max(a.fresh[b], 0) : 0;
-        const int h = (int)(((int64_t)c + a.page - 1) / a.page), w = (int)min(((int64_t)c + f + a.page - 1) / a.page, (int64_t)a.table_stride);
-        const int take = max(w - h, 0), ft = wave_scan(f), pt = wave_scan(take);
-        if ((tid & 63) == 63) wave_sum[0][tid >> 6] = ft, wave_sum[1][tid >> 6] = pt;
-        __syncthreads();
-        int fb = token_base, pb = page_base;
-        for (int i = 0; i < (tid >> 6); ++i) fb += wave_sum[0][i], pb += wave_sum[1][i];
-        for (int i = 0; i < kPlanThreads / 64; ++i) token_base += wave_sum[0][i], page_base += wave_sum[1][i];
-        tokens[tid] = fb + ft - f;
-        pages[tid] = pb + pt - take;
-        held[tid] = c;
-        have[tid] = h;
-        if (blockIdx.x == 0 && b < a.n_seqs) a.starts[b] = fb + ft - f;
-        if (tid == 0) tokens[kPlanThreads] = token_base;
-        if (b < a.n_seqs && b % gridDim.x == blockIdx.x)
-            for (int p = h; p < w; ++p) {
-                const int i = pb + pt - take + p - h;
-                a.table[(int64_t)b * a.table_stride + p] = i < a.n_free ? a.free_pages[i] : -1;
-            }
-        __syncthreads();
-        // slots of this chunk's tokens inside the block's range
-        const int64_t lo = max(s0, (int64_t)tokens[0]), hi = min(s1, (int64_t)token_base);
-        for (int64_t t = lo + tid; t < hi; t += kPlanThreads) {
-            int l = 0, r = kPlanThreads - 1;
-            while (l < r) {
-                const int mid = (l + r + 1) >> 1;
-                if (tokens[mid] <= t) l = mid; else r = mid - 1;
-            }
-            const int64_t at = (int64_t)held[l] + (t - tokens[l]), p = at / a.page;
-            int page = -1;
-            if (p < a.table_stride) {
-                if (p < have[l]) page = a.table[(int64_t)(b0 + l) * a.table_stride + p];
-                else {
-                    const int64_t i = pages[l] + (p - have[l]);
-                    if (i < a.n_free) page = a.free_pages[i];
-                }
-            }
-            a.slots[t] = page >= 0 ? (int64_t)page * a.page + at % a.page : -1;
+    const int64_t p0 = (int64_t)blockIdx.x * pages_per_block, p1 = (int)blockIdx.x == last ? INT32_MAX : p0 + pages_per_block;
+    int tokens_before = 0, pages_before = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += kPass) {
+        const int n = min(kPass, a.n_seqs - b0);
+        int c[kEach], f[kEach], take[kEach], sum_f = 0, sum_p = 0;
+        for (int i = 0; i < kEach; ++i) {
+            const int b = tid * kEach + i;
+            c[i] = b < n ? max(a.cached[b0 + b], 0) : 0;
+            f[i] = b < n ? max(a.fresh[b0 + b], 0) : 0;
         }
+        for (int i = 0; i < kEach; ++i) {
+            const int end = (int)min((int64_t)c[i] + f[i], (int64_t)INT32_MAX);
+            take[i] = max(min(pages_of(end, a.page, by_page), a.table_stride) - pages_of(c[i], a.page, by_page), 0);
+            sum_f += f[i];
+            sum_p += take[i];
+        }
+        int upto_f = sum_f, upto_p = sum_p;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int x = __shfl_up(upto_f, d), y = __shfl_up(upto_p, d);
+            if (lane >= d) upto_f += x, upto_p += y;
+        }
+        if (lane == 63) wave_sum[0][wave] = upto_f, wave_sum[1][wave] = upto_p;
+        __syncthreads();
+        int at_f = tokens_before + upto_f - sum_f, at_p = pages_before + upto_p - sum_p;
+        for (int w = 0; w < kThreads / 64; ++w) {
+            const int x = wave_sum[0][w], y = wave_sum[1][w];
+            if (w < wave) at_f += x, at_p += y;
+            tokens_before += x;
+            pages_before += y;
+        }
+        for (int i = 0; i < kEach; ++i) {
+            token[tid * kEach + i] = at_f;
+            taken[tid * kEach + i] = at_p;
+            held[tid * kEach + i] = c[i];
+            at_f += f[i];
+            at_p += take[i];
+        }
+        if (tid == kThreads - 1) token[kPass] = tokens_before, taken[kPass] = pages_before;
+        __syncthreads();
+        if (blockIdx.x == 0)
+            for (int b = tid; b < n; b += kThreads) a.starts[b0 + b] = token[b];
+        // pages of this pass in the block's share
+        const int64_t pe = min(p1, (int64_t)pages_before);
+        for (int64_t i = max(p0, (int64_t)taken[0]) + tid; i < pe; i += kThreads) {
+            const int b = holder(taken, n, (int)i);
+            a.table[(int64_t)(b0 + b) * a.table_stride + pages_of(held[b], a.page, by_page) + (i - taken[b])] = i < a.n_free ? a.free_pages[i] : -1;
+        }
+        // slots of this pass in the block's share
+        const int64_t se = min(s1, (int64_t)tokens_before);
+        int64_t t = max(s0, (int64_t)token[0]) + tid;
+        if (t < se)
+            for (int b = holder(token, n, (int)t); t < se; t += kSlots * kThreads) {
+                // some slots at a time, so that their pages' numbers are under way together
+                const int32_t *from[kSlots];
+                uint32_t place[kSlots];
+                int page[kSlots];
+                for (int k = 0; k < kSlots; ++k) {
+                    const int64_t tk = t + k * kThreads;
+                    from[k] = nullptr;
+                    if (tk >= se) continue;
+                    while (b + 1 < n && token[b + 1] <= tk) ++b;
+                    const uint32_t at = (uint32_t)held[b] + (uint32_t)(tk - token[b]), p = fdiv(at, by_page);
+                    place[k] = at - p * (uint32_t)a.page;
+                    if (p >= (uint32_t)a.table_stride) continue;
+                    const int have = pages_of(held[b], a.page, by_page);
+                    const int64_t i = (int64_t)taken[b] + p - have;
+                    if ((int)p < have) from[k] = a.table + (int64_t)(b0 + b) * a.table_stride + p;
+                    else if (i < a.n_free) from[k] = a.free_pages + i;
+                }
+                for (int k = 0; k < kSlots; ++k) page[k] = from[k] ? *from[k] : -1;
+                for (int k = 0; k < kSlots; ++k)
+                    if (t + k * kThreads < se) a.slots[t + k * kThreads] = page[k] >= 0 ? (int64_t)page[k] * a.page + place[k] : -1;
+            }
         __syncthreads();
     }
-    for (int64_t t = max(s0, (int64_t)token_base) + tid; t < s1; t += kPlanThreads) a.slots[t] = -1;
+    for (int64_t t = max(s0, (int64_t)tokens_before) + tid; t < s1; t += kThreads) a.slots[t] = -1;
     if (blockIdx.x == 0 && tid == 0) {
-        a.starts[a.n_seqs] = token_base;
-        a.counts[0] = token_base;
-        a.counts[1] = page_base;
+        a.starts[a.n_seqs] = tokens_before;
+        a.counts[0] = tokens_before;
+        a.counts[1] = pages_before;
     }
 }
 
-// one wave per row (token, head) of k (blockIdx.y = 0) or v
+// Copies of whole vectors: 16 bytes of k (blockIdx.y = 0) or v, kCopies of them a thread.  Bound by the bytes.
+constexpr int kCopies = 4;
+__global__ __launch_bounds__(256) void cache_copy(CacheStoreArgs a, FastDiv by_piece, FastDiv by_head, uint32_t n) {
+    const int pieces = a.head_dim >> 3;
+    const uint16_t *x = (const uint16_t *)(blockIdx.y ? a.v : a.k);
+    uint16_t *y = (uint16_t *)(blockIdx.y ? a.cache.v : a.cache.k);
+    const int64_t x_token = blockIdx.y ? a.v_token : a.k_token, x_head = blockIdx.y ? a.v_head : a.k_head;
+    v4u d[kCopies];
+    int64_t to[kCopies];
+    for (int i = 0; i < kCopies; ++i) {
+        const uint32_t at = (blockIdx.x * kCopies + i) * 256 + threadIdx.x;
+        to[i] = -1;
+        if (at >= n) continue;
+        const uint32_t row = fdiv(at, by_piece), piece = at - row * pieces, t = fdiv(row, by_head), h = row - t * a.kv_heads;
+        const int64_t slot = a.slots[t];
+        if (slot < 0 || slot >= (int64_t)a.cache.n_pages * a.cache.page) continue;
+        int64_t p;
+        if (slot < INT32_MAX) p = fdiv((uint32_t)slot, a.cache.by_page);
+        else p = slot / a.cache.page;
+        to[i] = p * a.cache.page_stride + (slot - p * a.cache.page) * a.cache.token_stride + h * a.cache.head_stride + piece * 8;
+        d[i] = *(const v4u *)(x + t * x_token + h * x_head + piece * 8);
+    }
+    for (int i = 0; i < kCopies; ++i)
+        if (to[i] >= 0) *(v4u *)(y + to[i]) = d[i];
+}
+
+// Codes of whole vectors: a group of 8 to 32 lanes a row, eight elements a lane, the maximum by exchanges inside the group.
+template <class T>
+__global__ __launch_bounds__(256) void cache_codes(CacheStoreArgs a, FastDiv by_head, int group_bits) {
+    typedef typename T::elem E;
+    const int lane = threadIdx.x & 63, piece = lane & ((1 << group_bits) - 1);
+    const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> group_bits;
+    if (r >= (int64_t)a.total * a.kv_heads) return;
+    const uint32_t t = fdiv((uint32_t)r, by_head), h = (uint32_t)r - t * a.kv_heads;
+    const int64_t slot = a.slots[t];
+    if (slot < 0 || slot >= (int64_t)a.cache.n_pages * a.cache.page) return;
+    const bool mine = piece * 8 < a.head_dim;
+    const E *x = blockIdx.y ? (const E *)a.v + t * a.v_token + h * a.v_head : (const E *)a.k + t * a.k_token + h * a.k_head;
+    typename T::v8 e = __builtin_bit_cast(typename T::v8, v4u{0, 0, 0, 0});
+    if (mine) e = *(const typename T::v8 *)(x + piece * 8);
+    float top = 0;
+    bool finite = true;
+    for (int i = 0; i < 8; ++i) {
+        const float v = fabsf((float)e[i]);
+        finite &= v < INFINITY;
+        top = fmaxf(top, v);
+    }
+    if (!finite) top = INFINITY;                                // (stays the group's maximum)
+    for (int d = 1 << group_bits >> 1; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float scale = top < INFINITY ? top * (1.f / 127.f) : __builtin_nanf("");
+    int64_t p;
+    if (slot < INT32_MAX) p = fdiv((uint32_t)slot, a.cache.by_page);
+    else p = slot / a.cache.page;
+    if (mine) {
+        uint32_t q[2] = {0, 0};
+        if (scale > 0.f)
+            for (int i = 0; i < 8; ++i) q[i >> 2] |= ((uint32_t)(int)fminf(fmaxf(rintf((float)e[i] / scale), -127.f), 127.f) & 255u) << (8 * (i & 3));
+        int8_t *y = (int8_t *)(blockIdx.y ? a.cache.v : a.cache.k) + p * a.cache.page_stride + (slot - p * a.cache.page) * a.cache.token_stride + h * a.cache.head_stride;
+        *(v2u *)(y + piece * 8) = v2u{q[0], q[1]};
+    }
+    if (piece == 0) (blockIdx.y ? a.cache.vs : a.cache.ks)[slot * a.kv_heads + h] = scale;
+}
+
+// any head dimension, stride and alignment: one wave per row (token, head) of k (blockIdx.y = 0) or v
 template <class T, bool CODES>
-__global__ __launch_bounds__(256) void cache_store(CacheStoreArgs a) {
+__global__ __launch_bounds__(256) void cache_store_any(CacheStoreArgs a) {
     typedef typename T::elem E;
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -109,23 +213,41 @@ __global__ __launch_bounds__(256) void cache_store(CacheStoreArgs a) {
 }  // namespace
 
 hawq_status launch_cache_plan(const CachePlanArgs &a, hipStream_t s) {
-    const int per = 1024;
-    const int64_t blocks = a.n_slots > 0 ? (a.n_slots + per - 1) / per : 1;
-    cache_plan<<<dim3((unsigned)blocks), kPlanThreads, 0, s>>>(a, per);
+    const int per = 4096;
+    const int64_t blocks = a.n_slots > per ? (a.n_slots + per - 1) / per : 1;
+    const int64_t pages = (a.n_slots / a.page + a.n_seqs + blocks - 1) / blocks;          // (a request's tokens may begin and end inside a page)
+    cache_plan<<<dim3((unsigned)blocks), kThreads, 0, s>>>(a, fast_div((uint32_t)a.page), per, (int)(pages < INT32_MAX ? pages : INT32_MAX));
     return check_launch();
 }
 
 hawq_status launch_cache_store(const CacheStoreArgs &a, hipStream_t s) {
-    const int64_t blocks = ((int64_t)a.total * a.kv_heads + 3) / 4;
+    const bool codes = a.cache.dtype == HAWQ_S8;
+    const int64_t rows = (int64_t)a.total * a.kv_heads;
+    const int64_t reads = a.k_token | a.k_head | a.v_token | a.v_head, writes = a.cache.page_stride | a.cache.token_stride | a.cache.head_stride;
+    const uintptr_t from = (uintptr_t)a.k | (uintptr_t)a.v, to = (uintptr_t)a.cache.k | (uintptr_t)a.cache.v;
+    if (a.head_dim % 8 == 0 && (reads | writes) % 8 == 0 && from % 16 == 0 && to % (codes ? 8 : 16) == 0 && rows * 32 < INT32_MAX) {
+        const FastDiv by_head = fast_div((uint32_t)a.kv_heads);
+        if (codes) {
+            int bits = 3;
+            while ((8 << bits) < a.head_dim) ++bits;
+            const dim3 grid((unsigned)(((rows << bits) + 255) / 256), 2);
+            if (a.dtype == HAWQ_F16) cache_codes<F16><<<grid, 256, 0, s>>>(a, by_head, bits);
+            else cache_codes<BF16><<<grid, 256, 0, s>>>(a, by_head, bits);
+        } else {
+            const uint32_t n = (uint32_t)(rows * (a.head_dim / 8));
+            cache_copy<<<dim3((n + 256 * kCopies - 1) / (256 * kCopies), 2), 256, 0, s>>>(a, fast_div((uint32_t)a.head_dim / 8), by_head, n);
+        }
+        return check_launch();
+    }
+    const int64_t blocks = (rows + 3) / 4;
     if (blocks > INT32_MAX) return HAWQ_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)blocks, 2);
-    const bool codes = a.cache.dtype == HAWQ_S8;
     if (a.dtype == HAWQ_F16) {
-        if (codes) cache_store<F16, true><<<grid, 256, 0, s>>>(a);
-        else cache_store<F16, false><<<grid, 256, 0, s>>>(a);
+        if (codes) cache_store_any<F16, true><<<grid, 256, 0, s>>>(a);
+        else cache_store_any<F16, false><<<grid, 256, 0, s>>>(a);
     } else {
-        if (codes) cache_store<BF16, true><<<grid, 256, 0, s>>>(a);
-        else cache_store<BF16, false><<<grid, 256, 0, s>>>(a);
+        if (codes) cache_store_any<BF16, true><<<grid, 256, 0, s>>>(a);
+        else cache_store_any<BF16, false><<<grid, 256, 0, s>>>(a);
     }
     return check_launch();
 }

@@ -63,58 +63,80 @@ template <class T, int RT, int MT, int PIECES, int ALIGN>
 __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_group) {
     typedef typename T::elem E;
     extern __shared__ __align__(16) char lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, r = lane & 15, c = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, r = lane & 15, c = lane >> 4;
     const int n0 = blockIdx.x * (16 * RT), m0 = blockIdx.y * (16 * MT);
     float *own = (float *)lds + wave * (RT * PIECES * 16 * 2);     // the wave's scales [tile][piece][2][16 outputs]
     const uint32_t flip = Nibbles<T>::base ^ (a.zeros ? 0u : Nibbles<T>::sign);
     const typename T::v8 ones = __builtin_bit_cast(typename T::v8, v4u{Nibbles<T>::one, Nibbles<T>::one, Nibbles<T>::one, Nibbles<T>::one});
 
-    // this lane's rows of w, scales and zero points, one for each tile, and its rows of x (past the last one: the last one again)
-    const uint8_t *w[RT], *z[RT];
-    const E *s[RT], *x[MT];
+    // Offsets of this lane's rows of w, scales and zero points, one for each tile, from the workgroup's first row, and of its rows of
+    // x (rows past the last one: the last one again).
+    uint32_t w_row[RT], s_row[RT], x_row[MT];
+    const int64_t first = (int64_t)n0;
     for (int t = 0; t < RT; ++t) {
-        const int64_t n = min(n0 + 16 * t + r, a.N - 1);
-        w[t] = a.w + n * (a.K >> 1);
-        s[t] = (const E *)a.scales + n * a.groups;
-        z[t] = a.zeros ? a.zeros + n * a.groups : nullptr;
+        const uint32_t n = min(16 * t + r, a.N - 1 - n0);
+        w_row[t] = n * (uint32_t)(a.K >> 1);
+        s_row[t] = n * (uint32_t)a.groups;
     }
-    for (int i = 0; i < MT; ++i) x[i] = (const E *)a.x + (int64_t)min(m0 + 16 * i + r, a.M - 1) * a.x_stride;
+    for (int i = 0; i < MT; ++i) x_row[i] = (uint32_t)min(16 * i + r, a.M - 1 - m0) * (uint32_t)a.x_stride;
+    const uint8_t *w0 = a.w + first * (a.K >> 1), *z0 = a.zeros ? a.zeros + first * a.groups : nullptr;
+    const E *s0 = (const E *)a.scales + first * a.groups, *x0 = (const E *)a.x + (int64_t)m0 * a.x_stride;
 
+    constexpr bool X_AHEAD = MT == 1;              // (x of more rows would not fit beside the next step's: read where it is used, from the caches)
     struct Stage {
-        v4u w[RT], x[MT][4];
+        v4u w[RT], x[X_AHEAD ? 1 : 0][4];
         E s[RT];
         uint8_t z[RT];
     };
+    auto load_x = [&](int k0, int i, v4u (&x)[4]) {
+        if (ALIGN == 16 && k0 + 128 <= a.K) {
+            for (int j = 0; j < 4; ++j) x[j] = *(const v4u *)(x0 + k0 + (x_row[i] + 32 * j + 8 * c));
+            return;
+        }
+        for (int j = 0; j < 4; ++j) {
+            const int k = k0 + 32 * j + 8 * c;
+            if constexpr (ALIGN > 1) {
+                x[j] = k < a.K ? *(const v4u *)(x0 + x_row[i] + k) : v4u{0, 0, 0, 0};
+            } else {
+                for (int e = 0; e < 4; ++e) {
+                    const uint16_t *p = (const uint16_t *)x0 + x_row[i] + k + 2 * e;
+                    x[j][e] = k + 2 * e < a.K ? p[0] | (uint32_t)p[1] << 16 : 0u;      // (K is even)
+                }
+            }
+        }
+    };
+    // the 128 weights from k0 on: 32 of this lane's rows from k0 + 32 c on
     auto load = [&](int k0, Stage &g) {
-        const int kw = k0 + 32 * c;                                 // the 32 weights this lane reads
-        const int group = (int)fdiv((uint32_t)min(kw, a.K - 1), by_group);
+        if (ALIGN == 16 && k0 + 128 <= a.K) {
+            const uint8_t *wk = w0 + (k0 >> 1);
+            const uint32_t group = PIECES == 1 ? fdiv((uint32_t)k0, by_group) : fdiv((uint32_t)(k0 + 32 * c), by_group);
+            for (int t = 0; t < RT; ++t) {
+                g.w[t] = *(const v4u *)(wk + (w_row[t] + 16 * c));
+                g.s[t] = s0[s_row[t] + group];
+                g.z[t] = z0 ? z0[s_row[t] + group] : 8;
+            }
+            if constexpr (X_AHEAD) load_x(k0, 0, g.x[0]);
+            return;
+        }
+        const int kw = k0 + 32 * c;
+        const uint32_t group = fdiv((uint32_t)min(kw, a.K - 1), by_group);
         for (int t = 0; t < RT; ++t) {
+            const uint8_t *wt = w0 + w_row[t];
             if constexpr (ALIGN == 16) {
-                g.w[t] = kw < a.K ? *(const v4u *)(w[t] + (kw >> 1)) : v4u{0, 0, 0, 0};
+                g.w[t] = kw < a.K ? *(const v4u *)(wt + (kw >> 1)) : v4u{0, 0, 0, 0};
             } else if constexpr (ALIGN == 4) {
-                for (int j = 0; j < 4; ++j) g.w[t][j] = kw + 8 * j < a.K ? *(const uint32_t *)(w[t] + ((kw + 8 * j) >> 1)) : 0u;
+                for (int j = 0; j < 4; ++j) g.w[t][j] = kw + 8 * j < a.K ? *(const uint32_t *)(wt + ((kw + 8 * j) >> 1)) : 0u;
             } else {
                 for (int j = 0; j < 4; ++j) {
                     uint32_t d = 0;
-                    for (int i = 0; i < 4; ++i) d |= (kw + 8 * j + 2 * i < a.K ? (uint32_t)w[t][(kw + 8 * j + 2 * i) >> 1] : 0u) << (8 * i);
+                    for (int i = 0; i < 4; ++i) d |= (kw + 8 * j + 2 * i < a.K ? (uint32_t)wt[(kw + 8 * j + 2 * i) >> 1] : 0u) << (8 * i);
                     g.w[t][j] = d;
                 }
             }
-            g.s[t] = s[t][group];
-            g.z[t] = z[t] ? z[t][group] : 8;
+            g.s[t] = s0[s_row[t] + group];
+            g.z[t] = z0 ? z0[s_row[t] + group] : 8;
         }
-        for (int i = 0; i < MT; ++i)
-            for (int j = 0; j < 4; ++j) {
-                const int k = k0 + 32 * j + 8 * c;
-                if constexpr (ALIGN > 1) {
-                    g.x[i][j] = k < a.K ? *(const v4u *)(x[i] + k) : v4u{0, 0, 0, 0};
-                } else {
-                    for (int e = 0; e < 4; ++e) {
-                        const uint16_t *p = (const uint16_t *)x[i] + k + 2 * e;
-                        g.x[i][j][e] = k + 2 * e < a.K ? p[0] | (uint32_t)p[1] << 16 : 0u;      // (K is even)
-                    }
-                }
-            }
+        if constexpr (X_AHEAD) load_x(k0, 0, g.x[0]);
     };
 
     v4f acc[RT][MT];
@@ -122,11 +144,12 @@ __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_grou
         for (int i = 0; i < MT; ++i) acc[t][i] = v4f{0, 0, 0, 0};
 
     const int steps = (a.K + 127) >> 7;
-    Stage now;
-    if (wave < steps) load(wave << 7, now);
-    for (int step = wave; step < steps; step += waves) {
-        Stage next;
-        if (step + waves < steps) load((step + waves) << 7, next);
+    auto use = [&](int k0, Stage &now) {
+        v4u xs[MT][4];
+        for (int i = 0; i < MT; ++i) {
+            if constexpr (X_AHEAD) for (int j = 0; j < 4; ++j) xs[i][j] = now.x[0][j];
+            else load_x(k0, i, xs[i]);
+        }
         // scales from a lane per output to a lane per four outputs (the accumulators' rows), through the wave's own LDS
         for (int t = 0; t < RT; ++t) {
             const int p = PIECES == 4 ? c : PIECES == 2 ? c >> 1 : 0;
@@ -141,7 +164,7 @@ __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_grou
             for (int p = 0; p < PIECES; ++p) {
                 v4f t{0, 0, 0, 0};
                 for (int j = p * 4 / PIECES; j < (p + 1) * 4 / PIECES; ++j) {
-                    xv[i][j] = ordered<T>(now.x[i][j]);
+                    xv[i][j] = ordered<T>(xs[i][j]);
                     t = T::mfma16(ones, xv[i][j], t);
                 }
                 sum[i][p] = t[0];
@@ -160,7 +183,18 @@ __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_grou
                     for (int e = 0; e < 4; ++e) acc[t][i][e] = fmaf(sc[e], part[i][e], fmaf(-sz[e], sum[i][p], acc[t][i][e]));
             }
         __builtin_amdgcn_wave_barrier();
-        now = next;
+    };
+    Stage even, odd;
+    int step = wave;
+    if (step < steps) load(step << 7, even);
+    while (step < steps) {
+        if (step + waves < steps) load((step + waves) << 7, odd);
+        use(step << 7, even);
+        step += waves;
+        if (step >= steps) break;
+        if (step + waves < steps) load((step + waves) << 7, even);
+        use(step << 7, odd);
+        step += waves;
     }
 
     // the waves' parts of 16 rows of y at a time: [wave][row][16 RT outputs, four more to spread the rows over the banks]
