@@ -410,7 +410,7 @@ hawq_status hawq_net_step_cost(const hawq_net *net, int32_t N, int32_t step, dou
  * uint8 [N, groups], values 0..15; scales T [N, groups], groups = ceil(K / group); bias T [N] or NULL.
  * x rows x_stride apart, y rows y_stride apart.  K even, group a positive multiple of 32 (the last group may be short).
  * Made for the rows of a decoding step, a few to some tens: the weights are read once for every 64 rows of x.
- * Any valid request is served; 16-byte aligned w and K a multiple of 32 read it in whole vectors.
+ * Any valid request with K up to 2^25 is served; 16-byte aligned w and K a multiple of 32 read it in whole vectors.
  */
 typedef struct {
     int32_t M, N, K;

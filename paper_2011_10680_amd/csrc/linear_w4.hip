@@ -18,6 +18,8 @@ namespace hawq {
 
 namespace {
 
+constexpr int kScaleBytes = 64 * 1024;       // of LDS for the scales of a segment of the reduction
+
 template <class T> struct Nibbles;
 template <> struct Nibbles<F16> {            // 16 + u: 0x4C00 | u << 6
     static constexpr uint32_t mask = 0x03C003C0u, base = 0x4C004C00u, sign = 0x02000200u, one = 0x3C003C00u;
@@ -28,14 +30,14 @@ template <> struct Nibbles<BF16> {           // 0x4180 | u << 3
     template <int I> static __device__ __forceinline__ uint32_t shift(uint32_t d) { return I == 0 ? d << 3 : I == 1 ? d >> 1 : I == 2 ? d >> 5 : d >> 9; }
 };
 
-// operand of eight weights: nibbles (0,4), (1,5), (2,6), (3,7)
+// operand of eight weights: nibbles (0,4), (1,5), (2,6), (3,7); base: Nibbles<T>::base ^ (sign where the weights are signed)
 template <class T>
-__device__ __forceinline__ typename T::v8 expand(uint32_t d, uint32_t flip) {
+__device__ __forceinline__ typename T::v8 expand(uint32_t d, uint32_t mask, uint32_t base) {
     v4u r;
-    r.x = (Nibbles<T>::template shift<0>(d) & Nibbles<T>::mask) ^ flip;
-    r.y = (Nibbles<T>::template shift<1>(d) & Nibbles<T>::mask) ^ flip;
-    r.z = (Nibbles<T>::template shift<2>(d) & Nibbles<T>::mask) ^ flip;
-    r.w = (Nibbles<T>::template shift<3>(d) & Nibbles<T>::mask) ^ flip;
+    r.x = (Nibbles<T>::template shift<0>(d) & mask) ^ base;
+    r.y = (Nibbles<T>::template shift<1>(d) & mask) ^ base;
+    r.z = (Nibbles<T>::template shift<2>(d) & mask) ^ base;
+    r.w = (Nibbles<T>::template shift<3>(d) & mask) ^ base;
     return __builtin_bit_cast(typename T::v8, r);
 }
 
@@ -58,83 +60,69 @@ __device__ __forceinline__ void exchange_quarters(v4u &d) {
 }
 
 // RT, MT: 16-output and 16-row tiles of a wave.  PIECES: parts of 128 weights with a scale of their own.  ALIGN: bytes the rows of w
-// are read in (16, 4; 1: also x element by element).
-template <class T, int RT, int MT, int PIECES, int ALIGN>
+// are read in (16, 4; 1: also x element by element).  ZEROS: unsigned weights with zero points.
+template <class T, int RT, int MT, int PIECES, int ALIGN, bool ZEROS>
 __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_group) {
     typedef typename T::elem E;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, r = lane & 15, c = lane >> 4;
     const int n0 = blockIdx.x * (16 * RT), m0 = blockIdx.y * (16 * MT);
-    float *own = (float *)lds + wave * (RT * PIECES * 16 * 2);     // the wave's scales [tile][piece][2][16 outputs]
-    const uint32_t flip = Nibbles<T>::base ^ (a.zeros ? 0u : Nibbles<T>::sign);
+    // scales of a segment of the reduction: [group][scale, scale * (16 + zero point)][outputs], fours of outputs swizzled by the group
+    constexpr int R = 16 * RT, SEG = kScaleBytes / (8 * R);
+    float *scale = (float *)lds;
+    auto swizzled = [&](int group, int row) { return row ^ ((group << 2) & (R - 1)); };
+    uint32_t mask = Nibbles<T>::mask, base = Nibbles<T>::base ^ (ZEROS ? 0u : Nibbles<T>::sign);
+    asm("" : "+s"(mask));                          // (registers: as literals the two operations would not be one instruction)
+    asm("" : "+v"(base));
     const typename T::v8 ones = __builtin_bit_cast(typename T::v8, v4u{Nibbles<T>::one, Nibbles<T>::one, Nibbles<T>::one, Nibbles<T>::one});
 
-    // Offsets of this lane's rows of w, scales and zero points, one for each tile, from the workgroup's first row, and of its rows of
-    // x (rows past the last one: the last one again).
-    uint32_t w_row[RT], s_row[RT], x_row[MT];
+    // Offsets of this lane's rows of w, one for each tile, from the workgroup's first row, and of its rows of x (rows past the last one:
+    // the last one again).
+    uint32_t w_row[RT];
+    std::conditional_t<ALIGN == 1, int64_t, uint32_t> x_row[MT];
     const int64_t first = (int64_t)n0;
     for (int t = 0; t < RT; ++t) {
-        const uint32_t n = min(16 * t + r, a.N - 1 - n0);
-        w_row[t] = n * (uint32_t)(a.K >> 1);
-        s_row[t] = n * (uint32_t)a.groups;
+        w_row[t] = (uint32_t)min(16 * t + r, a.N - 1 - n0) * (uint32_t)(a.K >> 1);
     }
-    for (int i = 0; i < MT; ++i) x_row[i] = (uint32_t)min(16 * i + r, a.M - 1 - m0) * (uint32_t)a.x_stride;
-    const uint8_t *w0 = a.w + first * (a.K >> 1), *z0 = a.zeros ? a.zeros + first * a.groups : nullptr;
+    for (int i = 0; i < MT; ++i) x_row[i] = min(16 * i + r, a.M - 1 - m0) * (decltype(x_row[0] + 0))a.x_stride;
+    const uint8_t *w0 = a.w + first * (a.K >> 1), *z0 = ZEROS ? a.zeros + first * a.groups : nullptr;
     const E *s0 = (const E *)a.scales + first * a.groups, *x0 = (const E *)a.x + (int64_t)m0 * a.x_stride;
 
-    constexpr bool X_AHEAD = MT == 1;              // (x of more rows would not fit beside the next step's: read where it is used, from the caches)
+    // x of more than 16 rows would not fit beside the next step's: it is read where it is used, from the caches
+    constexpr bool X_AHEAD = MT == 1;
     struct Stage {
         v4u w[RT], x[X_AHEAD ? 1 : 0][4];
-        E s[RT];
-        uint8_t z[RT];
     };
+    // No branches around loads: behind one the compiler no longer knows which loads are under way and waits for all of them.  What lies
+    // past the end of the reduction is read from its last whole piece, and x is zero there.
     auto load_x = [&](int k0, int i, v4u (&x)[4]) {
-        if (ALIGN == 16 && k0 + 128 <= a.K) {
-            for (int j = 0; j < 4; ++j) x[j] = *(const v4u *)(x0 + k0 + (x_row[i] + 32 * j + 8 * c));
-            return;
-        }
         for (int j = 0; j < 4; ++j) {
             const int k = k0 + 32 * j + 8 * c;
             if constexpr (ALIGN > 1) {
-                x[j] = k < a.K ? *(const v4u *)(x0 + x_row[i] + k) : v4u{0, 0, 0, 0};
+                x[j] = *(const v4u *)(x0 + (x_row[i] + (uint32_t)min(k, a.K - 8)));
             } else {
                 for (int e = 0; e < 4; ++e) {
-                    const uint16_t *p = (const uint16_t *)x0 + x_row[i] + k + 2 * e;
-                    x[j][e] = k + 2 * e < a.K ? p[0] | (uint32_t)p[1] << 16 : 0u;      // (K is even)
+                    const uint16_t *p = (const uint16_t *)x0 + (x_row[i] + (uint32_t)min(k + 2 * e, a.K - 2));
+                    x[j][e] = p[0] | (uint32_t)p[1] << 16;
                 }
             }
         }
     };
     // the 128 weights from k0 on: 32 of this lane's rows from k0 + 32 c on
     auto load = [&](int k0, Stage &g) {
-        if (ALIGN == 16 && k0 + 128 <= a.K) {
-            const uint8_t *wk = w0 + (k0 >> 1);
-            const uint32_t group = PIECES == 1 ? fdiv((uint32_t)k0, by_group) : fdiv((uint32_t)(k0 + 32 * c), by_group);
-            for (int t = 0; t < RT; ++t) {
-                g.w[t] = *(const v4u *)(wk + (w_row[t] + 16 * c));
-                g.s[t] = s0[s_row[t] + group];
-                g.z[t] = z0 ? z0[s_row[t] + group] : 8;
-            }
-            if constexpr (X_AHEAD) load_x(k0, 0, g.x[0]);
-            return;
-        }
         const int kw = k0 + 32 * c;
-        const uint32_t group = fdiv((uint32_t)min(kw, a.K - 1), by_group);
         for (int t = 0; t < RT; ++t) {
-            const uint8_t *wt = w0 + w_row[t];
             if constexpr (ALIGN == 16) {
-                g.w[t] = kw < a.K ? *(const v4u *)(wt + (kw >> 1)) : v4u{0, 0, 0, 0};
+                g.w[t] = *(const v4u *)(w0 + (w_row[t] + (uint32_t)(min(kw, a.K - 32) >> 1)));
             } else if constexpr (ALIGN == 4) {
-                for (int j = 0; j < 4; ++j) g.w[t][j] = kw + 8 * j < a.K ? *(const uint32_t *)(wt + ((kw + 8 * j) >> 1)) : 0u;
+                for (int j = 0; j < 4; ++j) g.w[t][j] = *(const uint32_t *)(w0 + (w_row[t] + (uint32_t)(min(kw + 8 * j, a.K - 8) >> 1)));
             } else {
                 for (int j = 0; j < 4; ++j) {
                     uint32_t d = 0;
-                    for (int i = 0; i < 4; ++i) d |= (kw + 8 * j + 2 * i < a.K ? (uint32_t)wt[(kw + 8 * j + 2 * i) >> 1] : 0u) << (8 * i);
+                    for (int i = 0; i < 4; ++i) d |= (uint32_t)w0[w_row[t] + (uint32_t)(min(kw + 8 * j + 2 * i, a.K - 2) >> 1)] << (8 * i);
                     g.w[t][j] = d;
                 }
             }
-            g.s[t] = s0[s_row[t] + group];
-            g.z[t] = z0 ? z0[s_row[t] + group] : 8;
         }
         if constexpr (X_AHEAD) load_x(k0, 0, g.x[0]);
     };
@@ -143,21 +131,17 @@ __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_grou
     for (int t = 0; t < RT; ++t)
         for (int i = 0; i < MT; ++i) acc[t][i] = v4f{0, 0, 0, 0};
 
-    const int steps = (a.K + 127) >> 7;
-    auto use = [&](int k0, Stage &now) {
+    auto use = [&](int k0, int g0, Stage &now) {
         v4u xs[MT][4];
         for (int i = 0; i < MT; ++i) {
             if constexpr (X_AHEAD) for (int j = 0; j < 4; ++j) xs[i][j] = now.x[0][j];
             else load_x(k0, i, xs[i]);
+            if (k0 + 128 > a.K)
+                for (int j = 0; j < 4; ++j)
+                    for (int e = 0; e < 4; ++e)
+                        if (k0 + 32 * j + 8 * c + 2 * e >= a.K) xs[i][j][e] = 0;
         }
-        // scales from a lane per output to a lane per four outputs (the accumulators' rows), through the wave's own LDS
-        for (int t = 0; t < RT; ++t) {
-            const int p = PIECES == 4 ? c : PIECES == 2 ? c >> 1 : 0;
-            const float sc = (float)now.s[t];
-            own[((t * PIECES + p) * 2 + 0) * 16 + r] = sc;
-            own[((t * PIECES + p) * 2 + 1) * 16 + r] = sc * (float)(16 + now.z[t]);
-            exchange_quarters(now.w[t]);
-        }
+        for (int t = 0; t < RT; ++t) exchange_quarters(now.w[t]);
         typename T::v8 xv[MT][4];
         float sum[MT][PIECES];                                      // (every row of the product with ones is the same)
         for (int i = 0; i < MT; ++i)
@@ -169,32 +153,46 @@ __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_grou
                 }
                 sum[i][p] = t[0];
             }
-        __builtin_amdgcn_wave_barrier();
+        int group[PIECES];                                          // of the segment
+        for (int p = 0; p < PIECES; ++p) group[p] = (int)fdiv((uint32_t)min(k0 + p * (128 / PIECES), a.K - 1), by_group) - g0;
         for (int t = 0; t < RT; ++t)
             for (int p = 0; p < PIECES; ++p) {
                 v4f part[MT];
                 for (int i = 0; i < MT; ++i) part[i] = v4f{0, 0, 0, 0};
                 for (int j = p * 4 / PIECES; j < (p + 1) * 4 / PIECES; ++j) {
-                    const typename T::v8 wv = expand<T>(now.w[t][j], flip);
+                    const typename T::v8 wv = expand<T>(now.w[t][j], mask, base);
                     for (int i = 0; i < MT; ++i) part[i] = T::mfma16(wv, xv[i][j], part[i]);
                 }
-                const v4f sc = *(const v4f *)(own + ((t * PIECES + p) * 2 + 0) * 16 + 4 * c), sz = *(const v4f *)(own + ((t * PIECES + p) * 2 + 1) * 16 + 4 * c);
+                const float *at = scale + group[p] * (2 * R) + swizzled(group[p], 16 * t + 4 * c);
+                const v4f sc = *(const v4f *)at, sz = *(const v4f *)(at + R);
                 for (int i = 0; i < MT; ++i)
                     for (int e = 0; e < 4; ++e) acc[t][i][e] = fmaf(sc[e], part[i][e], fmaf(-sz[e], sum[i][p], acc[t][i][e]));
             }
-        __builtin_amdgcn_wave_barrier();
     };
-    Stage even, odd;
-    int step = wave;
-    if (step < steps) load(step << 7, even);
-    while (step < steps) {
-        if (step + waves < steps) load((step + waves) << 7, odd);
-        use(step << 7, even);
-        step += waves;
-        if (step >= steps) break;
-        if (step + waves < steps) load((step + waves) << 7, even);
-        use(step << 7, odd);
-        step += waves;
+    for (int g0 = 0; g0 < a.groups; g0 += SEG) {
+        const int n_groups = min(SEG, a.groups - g0), last = (min(a.K, (g0 + n_groups) * a.group) + 127) >> 7;     // (SEG groups are whole steps)
+        int step = ((g0 * a.group) >> 7) + wave;
+        Stage even, odd;
+        load(min(step, last - 1) << 7, even);
+        if (g0 > 0) __syncthreads();
+        for (int row = wave; row < R; row += waves)
+            for (int g = lane; g < n_groups; g += 64) {
+                const uint32_t i = (uint32_t)min(row, a.N - 1 - n0) * (uint32_t)a.groups + g0 + g;
+                const float sc = (float)s0[i];
+                float *at = scale + g * (2 * R) + swizzled(g, row);
+                at[0] = sc;
+                at[R] = sc * (float)(16 + (ZEROS ? z0[i] : 8));
+            }
+        __syncthreads();
+        for (; step < last;) {
+            load(min(step + waves, last - 1) << 7, odd);
+            use(step << 7, g0, even);
+            step += waves;
+            if (step >= last) break;
+            load(min(step + waves, last - 1) << 7, even);
+            use(step << 7, g0, odd);
+            step += waves;
+        }
     }
 
     // the waves' parts of 16 rows of y at a time: [wave][row][16 RT outputs, four more to spread the rows over the banks]
@@ -220,10 +218,13 @@ __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_grou
 template <class T, int RT, int MT, int PIECES, int ALIGN>
 hawq_status launch(const LinearW4Args &a, hipStream_t s) {
     const int steps = (a.K + 127) / 128, waves = steps < 8 ? steps : 8;
-    const size_t scales = (size_t)waves * RT * PIECES * 16 * 2 * 4, sums = (size_t)waves * 16 * (16 * RT + 4) * 4;
+    const int segment = kScaleBytes / (8 * 16 * RT);
+    const size_t scales = (size_t)(a.groups < segment ? a.groups : segment) * 16 * RT * 8, sums = (size_t)waves * 16 * (16 * RT + 4) * 4;
     const dim3 grid((unsigned)((a.N + 16 * RT - 1) / (16 * RT)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
     if (grid.y > 65535) return HAWQ_ERR_UNSUPPORTED;
-    linear_w4<T, RT, MT, PIECES, ALIGN><<<grid, 64 * waves, scales > sums ? scales : sums, s>>>(a, fast_div((uint32_t)a.group));
+    const size_t lds = scales > sums ? scales : sums;
+    if (a.zeros) linear_w4<T, RT, MT, PIECES, ALIGN, true><<<grid, 64 * waves, lds, s>>>(a, fast_div((uint32_t)a.group));
+    else linear_w4<T, RT, MT, PIECES, ALIGN, false><<<grid, 64 * waves, lds, s>>>(a, fast_div((uint32_t)a.group));
     return check_launch();
 }
 
@@ -243,7 +244,7 @@ hawq_status pick_pieces(const LinearW4Args &a, hipStream_t s) {
 
 template <class T>
 hawq_status pick_align(const LinearW4Args &a, hipStream_t s) {
-    const bool x16 = ((uintptr_t)a.x & 15) == 0 && a.x_stride % 8 == 0;
+    const bool x16 = ((uintptr_t)a.x & 15) == 0 && a.x_stride % 8 == 0 && a.x_stride < (1 << 25);      // (32-bit offsets inside 64 rows)
     if (x16 && a.K % 32 == 0 && ((uintptr_t)a.w & 15) == 0) return pick_pieces<T, 16>(a, s);
     if (x16 && a.K % 8 == 0 && ((uintptr_t)a.w & 3) == 0) return pick_pieces<T, 4>(a, s);
     return pick_pieces<T, 1>(a, s);

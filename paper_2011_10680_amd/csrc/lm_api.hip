@@ -86,7 +86,7 @@ hawq_status hawq_linear_w4(const hawq_linear_w4_desc *d, const void *x, const vo
     if (d->w_dtype == HAWQ_S4 && zeros) return HAWQ_ERR_DTYPE;
     if (d->M == 0) return HAWQ_OK;      // (an empty tensor has no address)
     if (!x || !w || !scales || !y || (d->w_dtype == HAWQ_U4 && !zeros)) return HAWQ_ERR_NULL;
-    if (!at_multiple(2, {x, scales, bias, y})) return HAWQ_ERR_UNSUPPORTED;
+    if (!at_multiple(2, {x, scales, bias, y}) || d->K > (1 << 25)) return HAWQ_ERR_UNSUPPORTED;
     LinearW4Args a{x, scales, bias, (const uint8_t *)w, zeros, y, d->M, d->N, d->K, d->group, (int32_t)(((int64_t)d->K + d->group - 1) / d->group),
                    d->x_stride, d->y_stride, d->x_dtype};
     return launch_linear_w4(a, (hipStream_t)stream);
