@@ -184,34 +184,20 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
         float ks, vs;
         uint32_t seen;
     };
-    // Where a chunk's keys lie, in elements from the cache's start: this lane's key (lane & 31), or, WHOLE, the two tiles of 16
-    // keys; their scales' places; which keys are seen.  A key past the last one is the last one, not seen.
+    // The pages of a chunk's keys: that of this lane's key (lane & 31), or, WHOLE, those of the two tiles of 16 keys.  Only looked up
+    // here; a key past the last one is the last one, not seen.
     struct Place {
-        int64_t at[2], scale[2];
-        uint32_t seen;
+        int chunk, page[WHOLE ? 2 : 1];
     };
+    const Fixed<int32_t> table = (Fixed<int32_t>)keys.table;
     const int size = CODES ? 1 : 2;
+    auto key_of = [&](int chunk, int t) {                                             // first key of a tile, or this lane's key
+        const int j = chunk * kChunk + (WHOLE ? 16 * t : (lane & 31));
+        return WHOLE ? max(min(j, keys.cached - 1), 0) & ~15 : min(j, keys.cached - 1);
+    };
     auto look_up = [&](int chunk, Place &g) {
-        if constexpr (WHOLE) {
-            g.seen = 0;
-            for (int t = 0; t < 2; ++t) {
-                const int j = chunk * kChunk + 16 * t, n = min(keys.cached - j, 16), i = max(min(j, keys.cached - 1), 0) & ~15;
-                const int pg = (int)fdiv((uint32_t)i, a.cache.by_page), at = i - pg * a.cache.page, page = keys.table[pg];
-                const bool ok = (uint32_t)page < (uint32_t)a.cache.n_pages;
-                const int64_t good = ok ? page : 0;
-                g.at[t] = good * a.cache.page_stride + at * a.cache.token_stride + hk * a.cache.head_stride;
-                g.scale[t] = (good * a.cache.page + at) * a.kv_heads + hk;
-                if (ok && n > 0) g.seen |= (n == 16 ? 0xffffu : (1u << n) - 1) << (16 * t);
-            }
-        } else {
-            const int j = chunk * kChunk + (lane & 31), i = min(j, keys.cached - 1);
-            const int pg = (int)fdiv((uint32_t)i, a.cache.by_page), at = i - pg * a.cache.page, page = keys.table[pg];
-            const bool ok = (uint32_t)page < (uint32_t)a.cache.n_pages;
-            const int64_t good = ok ? page : 0;
-            g.at[0] = good * a.cache.page_stride + at * a.cache.token_stride + hk * a.cache.head_stride;
-            g.scale[0] = (good * a.cache.page + at) * a.kv_heads + hk;
-            g.seen = (uint32_t)__ballot(ok && j < keys.cached);
-        }
+        g.chunk = chunk;
+        for (int t = 0; t < (WHOLE ? 2 : 1); ++t) g.page[t] = table[fdiv((uint32_t)key_of(chunk, t), a.cache.by_page)];
     };
     // the lanes' loads: K a key and 16 bytes a lane; V a row's pieces side by side (past the head's elements: the first piece -- K's
     // meet zeros in q, V's are not stored)
@@ -225,46 +211,56 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
         const int d = CODES ? lane % LANES * 16 : ((lane % LANES) ^ f(i * V_ROWS + lane / LANES)) * 8;
         v_piece[i] = d < a.head_dim ? d : 0;
     }
+    const Global<char> k_cache = (Global<char>)a.cache.k, v_cache = (Global<char>)a.cache.v;
+    const int token_bytes = (int)a.cache.token_stride * size;                         // (WHOLE)
     auto load_cached = [&](const Place &w, Chunk &g, char *vt) {
-        g.seen = w.seen;
+        // elements from the cache's start and places of the scales, of a tile or of this lane's key
+        int64_t at[WHOLE ? 2 : 1], scale[WHOLE ? 2 : 1];
+        bool ok[WHOLE ? 2 : 1];
+        for (int t = 0; t < (WHOLE ? 2 : 1); ++t) {
+            const int i = key_of(w.chunk, t), place = i - (int)fdiv((uint32_t)i, a.cache.by_page) * a.cache.page;
+            ok[t] = (uint32_t)w.page[t] < (uint32_t)a.cache.n_pages;
+            const int64_t page = ok[t] ? w.page[t] : 0;
+            at[t] = (page * a.cache.page_stride + place * a.cache.token_stride + hk * a.cache.head_stride) * size;
+            scale[t] = (page * a.cache.page + place) * a.kv_heads + hk;
+        }
+        if constexpr (WHOLE) {
+            g.seen = 0;
+            for (int t = 0; t < 2; ++t) {
+                const int n = min(keys.cached - (w.chunk * kChunk + 16 * t), 16);
+                if (ok[t] && n > 0) g.seen |= (n == 16 ? 0xffffu : (1u << n) - 1) << (16 * t);
+            }
+        } else {
+            g.seen = (uint32_t)__ballot(ok[0] && w.chunk * kChunk + (lane & 31) < keys.cached);
+        }
         // row of a tile -> the row read: the last one seen where the tile is not full
         auto row_of = [&](int t, int row) {
-            if constexpr (WHOLE) {
-                const uint32_t seen = w.seen >> (16 * t) & 0xffffu;
-                return seen == 0xffffu ? row : min(row, max(31 - __builtin_clz(seen | 1u), 0));
-            }
-            return row;
-        };
-        auto base_of = [&](const void *p, int t) {                                    // WHOLE: one address for the tile, the same in every lane
-            const uint64_t at = (uint64_t)p + (uint64_t)(w.at[t] * size);
-            return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at) |
-                                  (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32);
+            const uint32_t seen = g.seen >> (16 * t) & 0xffffu;
+            return seen == 0xffffu ? row : min(row, 31 - __builtin_clz(seen | 1u));
         };
         if constexpr (CODES) {
-            const int64_t at = WHOLE ? ((lane & 16) ? w.scale[1] : w.scale[0]) + (int64_t)row_of((lane >> 4) & 1, lane & 15) * a.kv_heads : w.scale[0];
-            g.ks = a.cache.ks[at];
-            g.vs = a.cache.vs[at];
+            const int64_t i = WHOLE ? ((lane & 16) ? scale[1] : scale[0]) + (int64_t)row_of((lane >> 4) & 1, lane & 15) * a.kv_heads : scale[0];
+            g.ks = a.cache.ks[i];
+            g.vs = a.cache.vs[i];
         }
         for (int t = 0; t < 2; ++t) {
             if constexpr (WHOLE) {
-                const char *base = base_of(a.cache.k, t);
-                const int row = row_of(t, r) * (int)a.cache.token_stride;
-                for (int s = 0; s < K_LOADS; ++s) g.k[t][s] = *(const v4u *)(base + (uint32_t)((row + k_piece[s]) * size));
+                const uint32_t row = (uint32_t)(row_of(t, r) * token_bytes);
+                for (int s = 0; s < K_LOADS; ++s) g.k[t][s] = *(Global<v4u>)(k_cache + at[t] + (row + k_piece[s] * size));
             } else {
-                const int64_t at = shfl64(w.at[0], 16 * t + r);
-                for (int s = 0; s < K_LOADS; ++s) g.k[t][s] = *(const v4u *)((const char *)a.cache.k + (at + k_piece[s]) * size);
+                const int64_t key = shfl64(at[0], 16 * t + r);
+                for (int s = 0; s < K_LOADS; ++s) g.k[t][s] = *(Global<v4u>)(k_cache + key + k_piece[s] * size);
             }
         }
-        const char *v_base_of[2] = {WHOLE ? base_of(a.cache.v, 0) : nullptr, WHOLE ? base_of(a.cache.v, 1) : nullptr};
         for (int i = 0; i < N_V; ++i) {
-            const int row = i * V_ROWS + lane / LANES, piece = v_piece[i % (int)(sizeof(v_piece) / sizeof(int))];
-            const char *at;
+            const int row = i * V_ROWS + lane / LANES, piece = v_piece[i % (int)(sizeof(v_piece) / sizeof(int))] * size;
+            Global<char> from;
             if constexpr (WHOLE) {
                 const int t = i / (N_V / 2);
-                at = v_base_of[t] + (uint32_t)((row_of(t, row - 16 * t) * (int)a.cache.token_stride + piece) * size);
-            } else at = (const char *)a.cache.v + (shfl64(w.at[0], row) + piece) * size;
-            if constexpr (CODES) g.v[i] = *(const v4u *)at;
-            else __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)at, (__attribute__((address_space(3))) void *)(vt + i * 1024), 16, 0, 0);
+                from = v_cache + at[t] + (uint32_t)(row_of(t, row - 16 * t) * token_bytes + piece);
+            } else from = v_cache + shfl64(at[0], row) + piece;
+            if constexpr (CODES) g.v[i] = *(Global<v4u>)from;
+            else __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)(vt + i * 1024), 16, 0, 0);
         }
     };
 
@@ -395,33 +391,38 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
         char *ve = v_even + wave * RED, *vo = CODES ? ve : v_odd + wave * TILE;
         const int end = min(last, cached_chunks);
         int chunk = first + wave;
-        Place place;
-        Chunk even, odd;
         if (chunk < end) {
+            // Loads are issued without a branch around them (behind one the compiler waits for all that may be under way): a wave's last
+            // chunk is loaded once more, from the caches.
+            Place place;
+            Chunk even, odd;
             look_up(chunk, place);
             load_cached(place, even, ve);
-            if (chunk + W < end) look_up(chunk + W, place);
-        }
-        while (chunk < end) {
-            // (all loads of this chunk have landed; what is issued next is the following chunk's)
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            if (chunk + W < end) {
+            look_up(chunk + W < end ? chunk + W : chunk, place);
+            for (;;) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // all of this chunk has landed; what is issued next is the following one's
                 load_cached(place, odd, vo);
-                if (chunk + 2 * W < end) look_up(chunk + 2 * W, place);
-            }
-            use_cached(even, ve);
-            chunk += W;
-            if (chunk >= end) break;
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            if (chunk + W < end) {
+                look_up(chunk + 2 * W < end ? chunk + 2 * W : chunk, place);
+                use_cached(even, ve);
+                chunk += W;
+                if (chunk >= end) break;
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 load_cached(place, even, ve);
-                if (chunk + 2 * W < end) look_up(chunk + 2 * W, place);
+                look_up(chunk + 2 * W < end ? chunk + 2 * W : chunk, place);
+                use_cached(odd, vo);
+                chunk += W;
+                if (chunk >= end) break;
             }
-            use_cached(odd, vo);
-            chunk += W;
         }
         for (; chunk < last; chunk += W) use_drafts(chunk, ve);
     }
+
+    // From here on the arguments are read again where they are needed: held through the loop they would not fit the scalar registers.
+    Fixed<char> kernel_arguments = (Fixed<char>)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(kernel_arguments));
+    const AttnTreeArgs &late = *(const AttnTreeArgs *)kernel_arguments;
+    TreeKeys<T> rest(late, b, hk, 0);
+    rest.pad = keys.pad;
 
     // the waves join: each row's maximum and sum, then 16 rows' outputs at a time
     for (int n = 0; n < NT; ++n) {
@@ -453,7 +454,7 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
         __syncthreads();
         for (int e = threadIdx.x; e < 16 * (DP / 4); e += 64 * W) {
             const int i = e / (DP / 4), d = e % (DP / 4) * 4, row = row0 + 16 * n + i;
-            if (row >= n_rows || d >= a.head_dim) continue;
+            if (row >= n_rows || d >= late.head_dim) continue;
             v4f v{0, 0, 0, 0};
             for (int w = 0; w < W; ++w) v += *(const v4f *)(red + w * (RED / 4) + i * ROW + d);
             const float sum = joined[1][16 * n + i], any = v.x + v.y + v.z + v.w + sum;
@@ -463,11 +464,11 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
                 const float by = 1.f / sum;
                 typename T::v4 y;
                 for (int k = 0; k < 4; ++k) y[k] = (E)(sum == 0.f ? 0.f : v[k] * by);
-                *(typename T::v4 *)(keys.out(t, h) + d) = y;
+                *(typename T::v4 *)(rest.out(t, h) + d) = y;
             } else {
-                const int64_t at = part_of(a, p, keys.from + t, h, split);
-                *(v4f *)(a.partial + at * a.head_dim + d) = v;
-                if (d == 0) *(float2 *)(stats_of(a, p) + 2 * at) = make_float2(joined[0][16 * n + i], sum);
+                const int64_t at = part_of(late, p, rest.from + t, h, split);
+                *(v4f *)(late.partial + at * late.head_dim + d) = v;
+                if (d == 0) *(float2 *)(stats_of(late, p) + 2 * at) = make_float2(joined[0][16 * n + i], sum);
             }
         }
         __syncthreads();
@@ -478,14 +479,14 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
         for (uint32_t left = bad[half]; left; left &= left - 1, ++nth) {
             if (nth % W != wave) continue;
             const int row = row0 + 32 * half + __builtin_ctz(left), t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
-            const RowSums s = keys.attend(t, h, first * kChunk, last * kChunk, q_lds[wave]);
+            const RowSums s = rest.attend(t, h, first * kChunk, last * kChunk, q_lds[wave]);
             if (whole) {
-                store_row<T>(s, keys.out(t, h), a.head_dim);
+                store_row<T>(s, rest.out(t, h), late.head_dim);
             } else {
-                const int64_t i = part_of(a, p, keys.from + t, h, split);
+                const int64_t i = part_of(late, p, rest.from + t, h, split);
                 for (int k = 0; k < 4; ++k)
-                    if (lane + 64 * k < a.head_dim) a.partial[i * a.head_dim + lane + 64 * k] = s.total == 0.f ? 0.f : s.o[k];
-                if (lane < 2) stats_of(a, p)[2 * i + lane] = lane ? s.total : s.m * kLog2e;
+                    if (lane + 64 * k < late.head_dim) late.partial[i * late.head_dim + lane + 64 * k] = s.total == 0.f ? 0.f : s.o[k];
+                if (lane < 2) stats_of(late, p)[2 * i + lane] = lane ? s.total : s.m * kLog2e;
             }
         }
 }

@@ -97,6 +97,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t scalar_rsrc(const void *p, uin
     return __builtin_amdgcn_make_buffer_rsrc((void *)s, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 
+// Pointers that the compiler knows to be global memory (a pointer put together from integers is not known to be), and to data that
+// no kernel in flight writes, so that a load from the same place in every lane is a scalar one.
+template <class X> using Global = const __attribute__((address_space(1))) X *;
+template <class X> using Fixed = const __attribute__((address_space(4))) X *;
+
 // Rows [from, to) of sequence b, whatever the starts hold: inside [0, total) and not negative in number.
 __device__ __forceinline__ void sequence_rows(const int32_t *starts, int b, int total, int &from, int &to) {
     from = min(max(starts[b], 0), total);
