@@ -45,10 +45,40 @@ __global__ __launch_bounds__(64) void attn_prompt_any(AttnPromptArgs a) {
                  (E *)a.y + row * a.y_token + h * a.y_head, a.head_dim);
 }
 
-// The sequence and the 128 queries of tile `tile` (tiles of a sequence counted from its end: the longest rows first).  Every wave looks
-// for itself, 64 sequences at a time.
+// The sequence and the 128 queries of tile `tile`.  Every wave looks for itself.
+//
+// Up to 64 sequences the tiles are in falling order of their place in their sequence, whatever the sequence: the longest rows begin
+// first and the last workgroups to begin are the shortest.  A lane holds a sequence's number of tiles; the tiles at place p or
+// later number the sum of max(n - p, 0), and bisection finds the place whose tiles include this one.  More sequences are short ones
+// in the main: they follow one another, each from its end.
 __device__ __forceinline__ bool find_tile(const AttnPromptArgs &a, int tile, int &from, int &to, int &q0) {
     const int lane = threadIdx.x & 63;
+    if (a.n_seqs <= 64) {
+        int f = 0, t = 0;
+        if (lane < a.n_seqs) sequence_rows(a.starts, lane, a.total, f, t);
+        const int n = (t - f + kRows - 1) / kRows;
+        auto sum = [](int v) {
+            for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+            return __builtin_amdgcn_readfirstlane(v);
+        };
+        int most = n;
+        for (int d = 32; d > 0; d >>= 1) most = max(most, __shfl_xor(most, d));
+        int lo = 0, hi = __builtin_amdgcn_readfirstlane(most);             // tiles at place lo or later: more than `tile`; at hi or later: none
+        if (sum(n) <= tile) return false;
+        int past = 0;                                                       // tiles at place lo + 1 or later
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1, m = sum(max(n - mid, 0));
+            if (m > tile) lo = mid; else hi = mid, past = m;
+        }
+        // of the sequences with a tile at this place, the (tile - past)-th
+        uint64_t here = __ballot(n > lo);
+        for (int skip = tile - past; skip > 0; --skip) here &= here - 1;
+        const int l = __builtin_ctzll(here);
+        from = __builtin_amdgcn_readlane(f, l);
+        to = __builtin_amdgcn_readlane(t, l);
+        q0 = lo * kRows;
+        return true;
+    }
     int before = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
         int f = 0, t = 0;
@@ -143,10 +173,19 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(AttnPromptArgs a, float by
     auto compute = [&](int j0, const char *kt, const char *vt) {
         if (j0 > qw + 31) return;
         v16f sc[2];
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t)
             for (int e = 0; e < 16; ++e) sc[t][e] = 0;
-            for (int s = 0; s < KS; ++s) sc[t] = T::mfma32(*(const typename T::v8 *)(kt + k_at[s] + 32 * t * PITCH), q[s], sc[t]);
+        // (six of K's operands on their way before the first product, else each waits for its own: 1070 instead of 1045 TFLOP/s)
+        __builtin_amdgcn_sched_barrier(0);
+        for (int s = 0; s < KS; ++s)
+            for (int t = 0; t < 2; ++t) sc[t] = T::mfma32(*(const typename T::v8 *)(kt + k_at[s] + 32 * t * PITCH), q[s], sc[t]);
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+        for (int i = 0; i < 2 * KS - 6; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
+        __builtin_amdgcn_sched_barrier(0);
         if (j0 + kKeys - 1 > qw)
             for (int t = 0; t < 2; ++t)
                 for (int e = 0; e < 16; ++e)

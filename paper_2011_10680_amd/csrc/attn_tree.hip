@@ -1,6 +1,6 @@
 // Attention of drafted tokens over a paged cache and over one another.
 //
-// Matrix-core kernel.  The rows that share a key head (drafts x heads of the group) are taken 16, 32 or 64 to a workgroup, whose
+// Matrix-core kernel.  The rows that share a key head (drafts x heads of the group) are taken 16 or 32 to a workgroup, whose
 // waves walk over the cache 32 keys at a time, each wave every W-th of these chunks, and join their running maxima, sums and
 // outputs in LDS at the end; a long cache is shared out to several workgroups, whose parts a second launch joins.  As in prompt
 // attention the scores are computed transposed, S^T = K Q^T and O^T = V^T P^T: K's operand is read from memory straight into
@@ -71,11 +71,13 @@ __global__ __launch_bounds__(64) void attn_tree_any(AttnTreeArgs a) {
 }
 
 struct TreePlan {
-    int32_t rows;              // rows of a workgroup: 16, 32, 64
+    int32_t rows;              // rows of a workgroup: 16, 32
     int32_t row_tiles;         // workgroups over a request's rows
     int32_t waves;             // its waves
     int32_t chunks, splits;    // chunks of 32 keys of a workgroup, workgroups over a request's chunks at most
     FastDiv by_group;          // heads of a group
+    int32_t listed;            // up to 64 requests: workgroups take what work there is in turn, else one workgroup for all that might be
+    int32_t blocks;
 };
 
 constexpr int kChunk = 32;
@@ -84,15 +86,17 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
     TreePlan p;
     const int group = a.q_heads / a.kv_heads;
     const int64_t rows = (int64_t)a.max_drafts * group;
-    p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    p.rows = rows <= 16 ? 16 : 32;
     p.row_tiles = (int32_t)((rows + p.rows - 1) / p.rows);
     p.by_group = fast_div((uint32_t)group);
-    const int64_t most = (a.max_cached + kChunk - 1) / kChunk + (a.max_drafts + kChunk - 1) / kChunk, one = (int64_t)a.n_seqs * a.kv_heads * p.row_tiles;
+    const int64_t most = ((int64_t)a.max_cached + kChunk - 1) / kChunk + (a.max_drafts + kChunk - 1) / kChunk, one = (int64_t)a.n_seqs * a.kv_heads * p.row_tiles;
     // a cache of up to 1024 tokens: one workgroup of eight waves does it without a second launch
     p.waves = p.rows == 16 && most <= 33 ? 8 : 4;
     if (p.waves == 8) {
         p.chunks = (int32_t)most;
         p.splits = 1;
+        p.listed = 0;
+        p.blocks = (int32_t)one;
         return p;
     }
     // enough workgroups for every compute unit some times over (requests are of unequal length), but at least two chunks for a wave
@@ -100,6 +104,9 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
     chunks = (chunks + p.waves - 1) / p.waves * p.waves;
     p.chunks = (int32_t)(chunks < 2 * p.waves ? 2 * p.waves : chunks);
     p.splits = (int32_t)((most + p.chunks - 1) / p.chunks);
+    const int64_t all = one * p.splits, resident = 512;
+    p.listed = p.rows > 16 && a.n_seqs <= 64 && all > resident;
+    p.blocks = p.listed ? (int32_t)resident : all > INT32_MAX ? 0 : (int32_t)all;      // (0: too many)
     return p;
 }
 
@@ -141,23 +148,55 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
 // CODES: 8-bit cache.  WHOLE: every 16 keys of a chunk lie in one page.  DT: 32-element parts of the head dimension (2, 4).
 // NT: 16-row tiles.  W: waves.
 template <class T, bool CODES, bool WHOLE, int DT, int NT, int W>
-__global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArgs a, TreePlan p, float by_log2e, uint32_t negate) {
+__global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan p, float by_log2e, uint32_t negate) {
     typedef typename T::elem E;
     constexpr int PITCH = DT == 2 ? 128 : 256, D16 = 2 * DT, DP = 32 * DT, TILE = kChunk * PITCH, V_LOADS = TILE / 1024;
     constexpr int RED = 16 * (DP + 4) * 4 > TILE ? 16 * (DP + 4) * 4 : TILE;       // a wave's part of 16 rows, when the waves join
     __shared__ __align__(1024) char v_even[W * RED], v_odd[CODES ? 16 : W * TILE];   // (codes pass through registers: one buffer)
     __shared__ float scales[W][2][kChunk], stat[W][2][16 * NT], joined[2][16 * NT], q_lds[W][256];
-    __shared__ uint32_t bad[2];
+    __shared__ uint32_t bad;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane >> 4, r = lane & 15;
-    int id = blockIdx.x;
-    const int split = id % p.splits; id /= p.splits;
-    const int hk = id % a.kv_heads; id /= a.kv_heads;
-    const int tile = id % p.row_tiles, b = id / p.row_tiles;
+    const int group = a.q_heads / a.kv_heads;
+    // Work: key heads, row tiles, then parts of the cache of one request after the other.  Listed, a lane knows the work of the requests
+    // up to its own.
+    auto work_of = [&](int b, int &tiles) {
+        int from, to;
+        sequence_rows(a.starts, b, a.total, from, to);
+        const int drafts = min(to - from, a.max_drafts), chunks = (min(max(a.cached[b], 0), a.max_cached) + kChunk - 1) / kChunk + (drafts + kChunk - 1) / kChunk;
+        tiles = (drafts * group + 16 * NT - 1) / (16 * NT);
+        return drafts > 0 ? a.kv_heads * tiles * ((chunks + p.chunks - 1) / p.chunks) : 0;
+    };
+    const bool listed = NT > 1 && p.listed;
+    int upto = 0, my_tiles = 1, my_work = 0;
+    if (listed) {
+        if (lane < a.n_seqs) my_work = work_of(lane, my_tiles);
+        upto = my_work;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+    }
+    const int n_items = listed ? __builtin_amdgcn_readlane(upto, 63) : gridDim.x;
+    for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
+    int b, hk, tile, split, id = item;
+    if (listed) {
+        b = __builtin_ctzll(__ballot(upto > item));
+        id -= __builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(my_work, b);
+        const int tiles = __builtin_amdgcn_readlane(my_tiles, b);
+        hk = id % a.kv_heads; id /= a.kv_heads;
+        tile = id % tiles;
+        split = id / tiles;
+    } else {
+        hk = id % a.kv_heads; id /= a.kv_heads;
+        tile = id % p.row_tiles; id /= p.row_tiles;
+        split = id % p.splits;
+        b = id / p.splits;
+    }
     TreeKeys<T> keys(a, b, hk, 0);
-    const int group = a.q_heads / a.kv_heads, n_rows = keys.drafts * group, row0 = tile * 16 * NT;
+    const int n_rows = keys.drafts * group, row0 = tile * 16 * NT;
     const int cached_chunks = (keys.cached + kChunk - 1) / kChunk, n_chunks = cached_chunks + (keys.drafts + kChunk - 1) / kChunk;
     const int first = split * p.chunks, last = min(n_chunks, first + p.chunks);
-    if (row0 >= n_rows || first >= last) return;
+    if (row0 >= n_rows || first >= last) break;                    // (not listed: the only item)
     keys.pad = cached_chunks * kChunk;
 
     // queries: operand B; d of lane, step s: 32 s + 8 c, with codes 64 (s / 2) + 16 c + 8 (s % 2) (16 codes are one load)
@@ -432,7 +471,7 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
             stat[wave][1][16 * n + r] = total[n];
         }
     }
-    if (threadIdx.x < 2) bad[threadIdx.x] = 0;
+    if (threadIdx.x == 0) bad = 0;
     __syncthreads();
     if (threadIdx.x < 16 * NT) {
         float top = -INFINITY, sum = 0;
@@ -459,7 +498,7 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
             for (int w = 0; w < W; ++w) v += *(const v4f *)(red + w * (RED / 4) + i * ROW + d);
             const float sum = joined[1][16 * n + i], any = v.x + v.y + v.z + v.w + sum;
             const int t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
-            if (any != any) atomicOr(&bad[n >> 1], 1u << (16 * (n & 1) + i));
+            if (any != any) atomicOr(&bad, 1u << (16 * n + i));
             if (whole) {
                 const float by = 1.f / sum;
                 typename T::v4 y;
@@ -475,10 +514,9 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
     }
     // rows with a NaN once more, the plain way
     int nth = 0;
-    for (int half = 0; half < 2; ++half)
-        for (uint32_t left = bad[half]; left; left &= left - 1, ++nth) {
+        for (uint32_t left = bad; left; left &= left - 1, ++nth) {
             if (nth % W != wave) continue;
-            const int row = row0 + 32 * half + __builtin_ctz(left), t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
+            const int row = row0 + __builtin_ctz(left), t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
             const RowSums s = rest.attend(t, h, first * kChunk, last * kChunk, q_lds[wave]);
             if (whole) {
                 store_row<T>(s, rest.out(t, h), late.head_dim);
@@ -489,6 +527,9 @@ __global__ __launch_bounds__(64 * W, NT == 4 ? 1 : 2) void attn_tree(AttnTreeArg
                 if (lane < 2) stats_of(late, p)[2 * i + lane] = lane ? s.total : s.m * kLog2e;
             }
         }
+    if (!listed) break;
+    __syncthreads();
+    }
 }
 
 // one wave per row: the parts of a request that was shared out
@@ -516,12 +557,16 @@ __global__ __launch_bounds__(256) void attn_tree_join(AttnTreeArgs a, TreePlan p
             sum += w * stats[2 * s + 1];
         }
         const int here = min(64, n - s0);
-#pragma unroll 8
-        for (int i = 0; i < here; ++i) {
-            const float wi = __shfl(w, i);
-            const float2 x = *(const float2 *)(part + (int64_t)(s0 + i) * a.head_dim + two);
-            o.x += wi * x.x;
-            o.y += wi * x.y;
+        for (int i = 0; i < here; i += 8) {
+            float2 x[8];
+            for (int k = 0; k < 8; ++k) x[k] = *(const float2 *)(part + (int64_t)(s0 + min(i + k, here - 1)) * a.head_dim + two);
+            for (int k = 0; k < 8; ++k) {
+                const float wi = __shfl(w, min(i + k, 63));        // (0 past the last part)
+                if (i + k < here) {
+                    o.x += wi * x[k].x;
+                    o.y += wi * x[k].y;
+                }
+            }
         }
     }
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
@@ -539,36 +584,35 @@ bool matrix_form(const AttnTreeArgs &a) {
 }
 
 template <class T, bool CODES, bool WHOLE, int DT>
-void launch_rows(const AttnTreeArgs &a, const TreePlan &p, unsigned blocks, hipStream_t s) {
+void launch_rows(const AttnTreeArgs &a, const TreePlan &p, hipStream_t s) {
+    const unsigned blocks = (unsigned)p.blocks;
     const float c = fmaxf(fabsf(a.scale) * kLog2e, 1.2e-38f);       // (a negative scale: -q; zero: as good as the smallest number)
     const uint32_t negate = a.scale < 0 ? 0x80008000u : 0u;
     if (p.waves == 8) attn_tree<T, CODES, WHOLE, DT, 1, 8><<<blocks, 512, 0, s>>>(a, p, c, negate);
     else if (p.rows == 16) attn_tree<T, CODES, WHOLE, DT, 1, 4><<<blocks, 256, 0, s>>>(a, p, c, negate);
-    else if (p.rows == 32) attn_tree<T, CODES, WHOLE, DT, 2, 4><<<blocks, 256, 0, s>>>(a, p, c, negate);
-    else attn_tree<T, CODES, WHOLE, DT, 4, 4><<<blocks, 256, 0, s>>>(a, p, c, negate);
+    else attn_tree<T, CODES, WHOLE, DT, 2, 4><<<blocks, 256, 0, s>>>(a, p, c, negate);
 }
 
 template <class T, bool CODES>
-void launch_form(const AttnTreeArgs &a, const TreePlan &p, unsigned blocks, hipStream_t s) {
+void launch_form(const AttnTreeArgs &a, const TreePlan &p, hipStream_t s) {
     // 16 keys from a multiple of 16 on share a page; their rows lie within 31-bit offsets of the first
     if (a.cache.page % 16 == 0 && a.cache.token_stride < (1 << 25)) {
-        if (a.head_dim <= 64) launch_rows<T, CODES, true, 2>(a, p, blocks, s);
-        else launch_rows<T, CODES, true, 4>(a, p, blocks, s);
-    } else if (a.head_dim <= 64) launch_rows<T, CODES, false, 2>(a, p, blocks, s);
-    else launch_rows<T, CODES, false, 4>(a, p, blocks, s);
+        if (a.head_dim <= 64) launch_rows<T, CODES, true, 2>(a, p, s);
+        else launch_rows<T, CODES, true, 4>(a, p, s);
+    } else if (a.head_dim <= 64) launch_rows<T, CODES, false, 2>(a, p, s);
+    else launch_rows<T, CODES, false, 4>(a, p, s);
 }
 
 template <class T>
 hawq_status launch(const AttnTreeArgs &a, hipStream_t s) {
     const TreePlan p = tree_plan(a);
-    const int64_t blocks = (int64_t)a.n_seqs * a.kv_heads * p.row_tiles * p.splits;
     if (a.n_seqs > 65535 || a.q_heads > 65535) return HAWQ_ERR_UNSUPPORTED;
-    if (!matrix_form(a) || blocks > INT32_MAX) {
+    if (!matrix_form(a) || p.blocks == 0) {
         attn_tree_any<T><<<dim3((unsigned)a.max_drafts, (unsigned)a.q_heads, (unsigned)a.n_seqs), 64, 0, s>>>(a);
         return check_launch();
     }
-    if (a.cache.dtype == HAWQ_S8) launch_form<T, true>(a, p, (unsigned)blocks, s);
-    else launch_form<T, false>(a, p, (unsigned)blocks, s);
+    if (a.cache.dtype == HAWQ_S8) launch_form<T, true>(a, p, s);
+    else launch_form<T, false>(a, p, s);
     if (p.splits > 1) attn_tree_join<T><<<dim3((unsigned)(a.q_heads + 3) / 4, (unsigned)a.max_drafts, (unsigned)a.n_seqs), 256, 0, s>>>(a, p);
     return check_launch();
 }

@@ -14,21 +14,29 @@ __device__ __forceinline__ int pages_of(int n, int page, FastDiv by_page) {
     return q + (q * page < n);
 }
 
-// the last i < n with first[i] <= at (first[0] <= at): requests that get nothing share their neighbour's start and are passed over
-__device__ __forceinline__ int holder(const int *first, int n, int at) {
+// A request in LDS: the tokens and the pages given before it, the tokens it holds
+struct Request {
+    int token, taken, held, unused;
+};
+
+// the last i < n with token (PAGES: taken) of i not above at: requests that get nothing share their neighbour's start and are passed over
+template <bool PAGES>
+__device__ __forceinline__ int holder(const Request *r, int n, int at) {
     int lo = 0, hi = n - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (first[mid] <= at) lo = mid; else hi = mid - 1;
+        if ((PAGES ? r[mid].taken : r[mid].token) <= at) lo = mid; else hi = mid - 1;
     }
     return lo;
 }
 
 // Every workgroup adds up the tokens and pages of all requests (2048 in a pass: eight of a thread, then across the waves), so that one
 // launch does without an order among workgroups, and writes its own share of the slots and of the pages taken.  A thread finds
-// its first slot's request by bisection and walks on from there.  Bound by the slots' bytes, or by the chain of dependent steps.
+// its first slot's request by bisection and walks on from there with the request in registers.  Bound by the slots' bytes, or by
+// the chain of dependent steps.
 __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv by_page, int slots_per_block, int pages_per_block) {
-    __shared__ int token[kPass + 1], taken[kPass + 1], held[kPass], wave_sum[2][kThreads / 64];
+    __shared__ __align__(16) Request request[kPass + 1];
+    __shared__ int wave_sum[2][kThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, last = gridDim.x - 1;
     const int64_t s0 = (int64_t)blockIdx.x * slots_per_block, s1 = min(s0 + slots_per_block, a.n_slots);
     const int64_t p0 = (int64_t)blockIdx.x * pages_per_block, p1 = (int)blockIdx.x == last ? INT32_MAX : p0 + pages_per_block;
@@ -37,11 +45,14 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
         const int n = min(kPass, a.n_seqs - b0);
         int c[kEach], f[kEach], take[kEach], sum_f = 0, sum_p = 0;
         for (int i = 0; i < kEach; ++i) {
-            const int b = tid * kEach + i;
-            c[i] = b < n ? max(a.cached[b0 + b], 0) : 0;
-            f[i] = b < n ? max(a.fresh[b0 + b], 0) : 0;
+            const int b = tid * kEach + i, at = b0 + min(b, n - 1);
+            c[i] = a.cached[at];
+            f[i] = a.fresh[at];
         }
         for (int i = 0; i < kEach; ++i) {
+            const bool is = tid * kEach + i < n;
+            c[i] = is ? max(c[i], 0) : 0;
+            f[i] = is ? max(f[i], 0) : 0;
             const int end = (int)min((int64_t)c[i] + f[i], (int64_t)INT32_MAX);
             take[i] = max(min(pages_of(end, a.page, by_page), a.table_stride) - pages_of(c[i], a.page, by_page), 0);
             sum_f += f[i];
@@ -54,6 +65,7 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
         }
         if (lane == 63) wave_sum[0][wave] = upto_f, wave_sum[1][wave] = upto_p;
         __syncthreads();
+        const int first_token = tokens_before, first_page = pages_before;
         int at_f = tokens_before + upto_f - sum_f, at_p = pages_before + upto_p - sum_p;
         for (int w = 0; w < kThreads / 64; ++w) {
             const int x = wave_sum[0][w], y = wave_sum[1][w];
@@ -62,27 +74,29 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
             pages_before += y;
         }
         for (int i = 0; i < kEach; ++i) {
-            token[tid * kEach + i] = at_f;
-            taken[tid * kEach + i] = at_p;
-            held[tid * kEach + i] = c[i];
+            request[tid * kEach + i] = {at_f, at_p, c[i], 0};
             at_f += f[i];
             at_p += take[i];
         }
-        if (tid == kThreads - 1) token[kPass] = tokens_before, taken[kPass] = pages_before;
+        if (tid == kThreads - 1) request[kPass] = {tokens_before, pages_before, 0, 0};
         __syncthreads();
         if (blockIdx.x == 0)
-            for (int b = tid; b < n; b += kThreads) a.starts[b0 + b] = token[b];
+            for (int b = tid; b < n; b += kThreads) a.starts[b0 + b] = request[b].token;
         // pages of this pass in the block's share
         const int64_t pe = min(p1, (int64_t)pages_before);
-        for (int64_t i = max(p0, (int64_t)taken[0]) + tid; i < pe; i += kThreads) {
-            const int b = holder(taken, n, (int)i);
-            a.table[(int64_t)(b0 + b) * a.table_stride + pages_of(held[b], a.page, by_page) + (i - taken[b])] = i < a.n_free ? a.free_pages[i] : -1;
+        for (int64_t i = max(p0, (int64_t)first_page) + tid; i < pe; i += kThreads) {
+            const int page = i < a.n_free ? a.free_pages[i] : -1, b = holder<true>(request, n, (int)i);
+            const Request r = request[b];
+            a.table[(int64_t)(b0 + b) * a.table_stride + pages_of(r.held, a.page, by_page) + (i - r.taken)] = page;
         }
         // slots of this pass in the block's share
         const int64_t se = min(s1, (int64_t)tokens_before);
-        int64_t t = max(s0, (int64_t)token[0]) + tid;
-        if (t < se)
-            for (int b = holder(token, n, (int)t); t < se; t += kSlots * kThreads) {
+        int64_t t = max(s0, (int64_t)first_token) + tid;
+        if (t < se) {
+            int b = holder<false>(request, n, (int)t);
+            Request r = request[b];
+            int next = request[b + 1].token, have = pages_of(r.held, a.page, by_page);
+            for (; t < se; t += kSlots * kThreads) {
                 // some slots at a time, so that their pages' numbers are under way together
                 const int32_t *from[kSlots];
                 uint32_t place[kSlots];
@@ -91,12 +105,16 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
                     const int64_t tk = t + k * kThreads;
                     from[k] = nullptr;
                     if (tk >= se) continue;
-                    while (b + 1 < n && token[b + 1] <= tk) ++b;
-                    const uint32_t at = (uint32_t)held[b] + (uint32_t)(tk - token[b]), p = fdiv(at, by_page);
+                    if (next <= tk && b + 1 < n) {
+                        do ++b; while (b + 1 < n && request[b + 1].token <= tk);
+                        r = request[b];
+                        next = request[b + 1].token;
+                        have = pages_of(r.held, a.page, by_page);
+                    }
+                    const uint32_t at = (uint32_t)r.held + (uint32_t)(tk - r.token), p = fdiv(at, by_page);
                     place[k] = at - p * (uint32_t)a.page;
                     if (p >= (uint32_t)a.table_stride) continue;
-                    const int have = pages_of(held[b], a.page, by_page);
-                    const int64_t i = (int64_t)taken[b] + p - have;
+                    const int64_t i = (int64_t)r.taken + p - have;
                     if ((int)p < have) from[k] = a.table + (int64_t)(b0 + b) * a.table_stride + p;
                     else if (i < a.n_free) from[k] = a.free_pages + i;
                 }
@@ -104,6 +122,7 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
                 for (int k = 0; k < kSlots; ++k)
                     if (t + k * kThreads < se) a.slots[t + k * kThreads] = page[k] >= 0 ? (int64_t)page[k] * a.page + place[k] : -1;
             }
+        }
         __syncthreads();
     }
     for (int64_t t = max(s0, (int64_t)tokens_before) + tid; t < s1; t += kThreads) a.slots[t] = -1;
