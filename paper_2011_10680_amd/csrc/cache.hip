@@ -5,7 +5,7 @@ namespace hawq {
 
 namespace {
 
-constexpr int kThreads = 256, kEach = 8, kPass = kThreads * kEach;    // requests of a thread and of a pass
+constexpr int kThreads = 1024, kEach = 2, kPass = kThreads * kEach;   // requests of a thread and of a pass
 constexpr int kSlots = 8;                                             // slots of a thread under way
 
 // ceil(n / page) for n < 2^31
@@ -30,7 +30,7 @@ __device__ __forceinline__ int holder(const Request *r, int n, int at) {
     return lo;
 }
 
-// Every workgroup adds up the tokens and pages of all requests (2048 in a pass: eight of a thread, then across the waves), so that one
+// Every workgroup adds up the tokens and pages of all requests (2048 in a pass: two of a thread, then across the waves), so that one
 // launch does without an order among workgroups, and writes its own share of the slots and of the pages taken.  A thread finds
 // its first slot's request by bisection and walks on from there with the request in registers.  Bound by the slots' bytes, or by
 // the chain of dependent steps.
@@ -40,14 +40,20 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, last = gridDim.x - 1;
     const int64_t s0 = (int64_t)blockIdx.x * slots_per_block, s1 = min(s0 + slots_per_block, a.n_slots);
     const int64_t p0 = (int64_t)blockIdx.x * pages_per_block, p1 = (int)blockIdx.x == last ? INT32_MAX : p0 + pages_per_block;
+    const bool vectors = (((uintptr_t)a.cached | (uintptr_t)a.fresh) & 7) == 0;
     int tokens_before = 0, pages_before = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += kPass) {
         const int n = min(kPass, a.n_seqs - b0);
         int c[kEach], f[kEach], take[kEach], sum_f = 0, sum_p = 0;
-        for (int i = 0; i < kEach; ++i) {
-            const int b = tid * kEach + i, at = b0 + min(b, n - 1);
-            c[i] = a.cached[at];
-            f[i] = a.fresh[at];
+        if (vectors && tid * kEach + kEach <= n) {
+            *(v2i *)c = *(const v2i *)(a.cached + b0 + tid * kEach);
+            *(v2i *)f = *(const v2i *)(a.fresh + b0 + tid * kEach);
+        } else {
+            for (int i = 0; i < kEach; ++i) {
+                const int at = b0 + min(tid * kEach + i, n - 1);
+                c[i] = a.cached[at];
+                f[i] = a.fresh[at];
+            }
         }
         for (int i = 0; i < kEach; ++i) {
             const bool is = tid * kEach + i < n;
@@ -232,10 +238,11 @@ __global__ __launch_bounds__(256) void cache_store_any(CacheStoreArgs a) {
 }  // namespace
 
 hawq_status launch_cache_plan(const CachePlanArgs &a, hipStream_t s) {
-    const int per = 4096;
+    // one workgroup for a compute unit at most: each reads all lengths, and a thousand that read the same lines wait for one another
+    const int64_t share = (a.n_slots + 255) / 256, per = share < kThreads ? kThreads : (share + kThreads - 1) / kThreads * kThreads;
     const int64_t blocks = a.n_slots > per ? (a.n_slots + per - 1) / per : 1;
     const int64_t pages = (a.n_slots / a.page + a.n_seqs + blocks - 1) / blocks;          // (a request's tokens may begin and end inside a page)
-    cache_plan<<<dim3((unsigned)blocks), kThreads, 0, s>>>(a, fast_div((uint32_t)a.page), per, (int)(pages < INT32_MAX ? pages : INT32_MAX));
+    cache_plan<<<dim3((unsigned)blocks), kThreads, 0, s>>>(a, fast_div((uint32_t)a.page), (int)per, (int)(pages < INT32_MAX ? pages : INT32_MAX));
     return check_launch();
 }
 
