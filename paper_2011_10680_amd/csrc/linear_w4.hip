@@ -228,13 +228,18 @@ hawq_status launch(const LinearW4Args &a, hipStream_t s) {
     return check_launch();
 }
 
+// Tiles: as many outputs to a workgroup as still leave about 200 workgroups, since every workgroup reads all of x; more than 32
+// rows in two halves where that makes up for outputs.  Measured (K = 8192, or 4096 below 8192 outputs; us for 16, 32 and 64 outputs a
+// workgroup): 13 rows of 16384 40 / 27 / 25, 30 rows of 4096 10.7 / 13.2 / 17.9, of 8192 34 / 22 / 29, of 16384 64 / 40 / 30; 64 rows of
+// 8192 67 / 39 / 45, of 16384 134 / 76 / 47; in halves 64 rows of 2048 11.3 / 13.0 (whole 18.9), of 4096 19.5 / 13.9 (whole 19.4).
 template <class T, int PIECES, int ALIGN>
 hawq_status pick_tiles(const LinearW4Args &a, hipStream_t s) {
     if constexpr (ALIGN == 16) {
-        if (a.N >= 64 * 192) return a.M <= 16 ? launch<T, 4, 1, PIECES, ALIGN>(a, s) : a.M <= 32 ? launch<T, 4, 2, PIECES, ALIGN>(a, s) : launch<T, 2, 4, PIECES, ALIGN>(a, s);
+        if (a.N >= 64 * 192) return a.M <= 16 ? launch<T, 4, 1, PIECES, ALIGN>(a, s) : a.M <= 32 ? launch<T, 4, 2, PIECES, ALIGN>(a, s) : launch<T, 4, 4, PIECES, ALIGN>(a, s);
         if (a.N >= 32 * 192) return a.M <= 16 ? launch<T, 2, 1, PIECES, ALIGN>(a, s) : a.M <= 32 ? launch<T, 2, 2, PIECES, ALIGN>(a, s) : launch<T, 2, 4, PIECES, ALIGN>(a, s);
+        if (a.N >= 32 * 96 && a.M > 32) return launch<T, 2, 2, PIECES, ALIGN>(a, s);
     }
-    return a.M <= 16 ? launch<T, 1, 1, PIECES, ALIGN>(a, s) : launch<T, 1, 4, PIECES, ALIGN>(a, s);
+    return a.M <= 16 ? launch<T, 1, 1, PIECES, ALIGN>(a, s) : launch<T, 1, 2, PIECES, ALIGN>(a, s);
 }
 
 template <class T, int ALIGN>
