@@ -28,7 +28,7 @@ struct TreeKeys {
     int hk, from, drafts, cached, pad;
     const int32_t *table;
 
-    __device__ __forceinline__ TreeKeys(const AttnTreeArgs &args, int b, int head, int first) : a(args), hk(head), from(first) {
+    __device__ __forceinline__ TreeKeys(const AttnTreeArgs &args, int b, int head) : a(args), hk(head) {
         int to;
         sequence_rows(a.starts, b, a.total, from, to);
         drafts = min(to - from, a.max_drafts);
@@ -36,6 +36,7 @@ struct TreeKeys {
         pad = cached;
         table = a.table + (int64_t)b * a.table_stride;
     }
+    __device__ __forceinline__ TreeKeys(const AttnTreeArgs &args, const TreeKeys &k) : a(args), hk(k.hk), from(k.from), drafts(k.drafts), cached(k.cached), pad(k.pad), table(k.table) {}
     __device__ __forceinline__ bool on_a_page(int j) const { return (uint32_t)table[fdiv((uint32_t)j, a.cache.by_page)] < (uint32_t)a.cache.n_pages; }
     __device__ __forceinline__ uint64_t mask(int t) const { return a.mask ? a.mask[from + t] : t == 63 ? ~0ull : (2ull << t) - 1; }
     __device__ __forceinline__ KeyRow operator()(int j) const {
@@ -65,7 +66,7 @@ template <class T>
 __global__ __launch_bounds__(64) void attn_tree_any(AttnTreeArgs a) {
     __shared__ float q_lds[256];
     const int t = blockIdx.x, h = blockIdx.y;
-    const TreeKeys<T> keys(a, blockIdx.z, h / (a.q_heads / a.kv_heads), 0);
+    const TreeKeys<T> keys(a, blockIdx.z, h / (a.q_heads / a.kv_heads));
     if (t >= keys.drafts) return;
     store_row<T>(keys.attend(t, h, 0, keys.cached + keys.drafts, q_lds), keys.out(t, h), a.head_dim);
 }
@@ -74,9 +75,9 @@ struct TreePlan {
     int32_t rows;              // rows of a workgroup: 16, 32
     int32_t row_tiles;         // workgroups over a request's rows
     int32_t waves;             // its waves
-    int32_t chunks, splits;    // chunks of 32 keys of a workgroup, workgroups over a request's chunks at most
+    int32_t chunks, splits;    // chunks of 32 keys of a workgroup (listed: at least), workgroups over a request's chunks at most
     FastDiv by_group;          // heads of a group
-    int32_t listed;            // up to 64 requests: workgroups take what work there is in turn, else one workgroup for all that might be
+    int32_t listed;            // workgroups take what work there is in turn, else one workgroup for all that might be
     int32_t blocks;
 };
 
@@ -90,22 +91,23 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
     p.row_tiles = (int32_t)((rows + p.rows - 1) / p.rows);
     p.by_group = fast_div((uint32_t)group);
     const int64_t most = ((int64_t)a.max_cached + kChunk - 1) / kChunk + (a.max_drafts + kChunk - 1) / kChunk, one = (int64_t)a.n_seqs * a.kv_heads * p.row_tiles;
-    // a cache of up to 1024 tokens: one workgroup of eight waves does it without a second launch
-    p.waves = p.rows == 16 && most <= 33 ? 8 : 4;
-    if (p.waves == 8) {
+    // caches of up to 1024 tokens are not shared out (no second launch): a workgroup has eight waves where there are few of them
+    p.waves = p.rows == 16 && most <= 33 && one <= 256 ? 8 : 4;
+    if (most <= 33 && (p.waves == 8 || one >= 256)) {
         p.chunks = (int32_t)most;
         p.splits = 1;
         p.listed = 0;
-        p.blocks = (int32_t)one;
+        p.blocks = one > INT32_MAX ? 0 : (int32_t)one;
         return p;
     }
-    // enough workgroups for every compute unit some times over (requests are of unequal length), but at least two chunks for a wave
-    int64_t chunks = (most * one + 4095) / 4096;
+    // At least two chunks for a wave.  With 32 rows and up to 64 requests the kernel itself sizes the parts; else enough workgroups for
+    // every compute unit some times over, since the requests are of unequal length.
+    int64_t chunks = p.rows > 16 && a.n_seqs <= 64 ? 1 : (most * one + 4095) / 4096;
     chunks = (chunks + p.waves - 1) / p.waves * p.waves;
     p.chunks = (int32_t)(chunks < 2 * p.waves ? 2 * p.waves : chunks);
     p.splits = (int32_t)((most + p.chunks - 1) / p.chunks);
     const int64_t all = one * p.splits, resident = 512;
-    p.listed = p.rows > 16 && a.n_seqs <= 64 && all > resident;
+    p.listed = p.rows > 16 && a.n_seqs <= 64 && all > resident && p.splits > 1;
     p.blocks = p.listed ? (int32_t)resident : all > INT32_MAX ? 0 : (int32_t)all;      // (0: too many)
     return p;
 }
@@ -113,6 +115,12 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
 // partial sums: [row][q head][split][head_dim] floats, then [row][q head][split][2]: maximum (powers of two) and sum of weights
 __device__ __forceinline__ int64_t part_of(const AttnTreeArgs &a, const TreePlan &p, int64_t row, int h, int split) { return (row * a.q_heads + h) * p.splits + split; }
 __device__ __forceinline__ float *stats_of(const AttnTreeArgs &a, const TreePlan &p) { return a.partial + (int64_t)a.total * a.q_heads * p.splits * a.head_dim; }
+// behind them the chunks of a part, where the work is listed
+__device__ __forceinline__ int *chunks_of(const AttnTreeArgs &a, const TreePlan &p) { return (int *)(stats_of(a, p) + (int64_t)a.total * a.q_heads * p.splits * 2); }
+__device__ __forceinline__ int sum_of_lanes(int v) {
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    return __builtin_amdgcn_readfirstlane(v);
+}
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
@@ -158,23 +166,31 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane >> 4, r = lane & 15;
     const int group = a.q_heads / a.kv_heads;
     // Work: key heads, row tiles, then parts of the cache of one request after the other.  Listed, a lane knows the work of the requests
-    // up to its own.
-    auto work_of = [&](int b, int &tiles) {
-        int from, to;
-        sequence_rows(a.starts, b, a.total, from, to);
-        const int drafts = min(to - from, a.max_drafts), chunks = (min(max(a.cached[b], 0), a.max_cached) + kChunk - 1) / kChunk + (drafts + kChunk - 1) / kChunk;
-        tiles = (drafts * group + 16 * NT - 1) / (16 * NT);
-        return drafts > 0 ? a.kv_heads * tiles * ((chunks + p.chunks - 1) / p.chunks) : 0;
-    };
-    const bool listed = NT > 1 && p.listed;
-    int upto = 0, my_tiles = 1, my_work = 0;
+    // up to its own, and a part is as many chunks as give every workgroup one.
+    const bool listed = NT > 1 && p.listed;      // (16 rows: shorter parts and no list measured 141 us where lists took 157, decode of 32 requests)
+    int chunks = p.chunks, upto = 0, my_tiles = 1, my_work = 0;
     if (listed) {
-        if (lane < a.n_seqs) my_work = work_of(lane, my_tiles);
+        int my_chunks = 0;
+        if (lane < a.n_seqs) {
+            int from, to;
+            sequence_rows(a.starts, lane, a.total, from, to);
+            const int drafts = min(to - from, a.max_drafts), cached = min(max(a.cached[lane], 0), a.max_cached);
+            my_tiles = (drafts * group + 16 * NT - 1) / (16 * NT);
+            my_chunks = drafts > 0 ? (cached + kChunk - 1) / kChunk + (drafts + kChunk - 1) / kChunk : 0;
+        }
+        float all = (float)a.kv_heads * (float)my_tiles * (float)my_chunks;
+        for (int d = 32; d > 0; d >>= 1) all += __shfl_xor(all, d);
+        chunks = max(chunks, __builtin_amdgcn_readfirstlane((int)(all / (float)gridDim.x) / W * W + W));
+        for (;; chunks += (chunks / 8 + W) / W * W) {
+            my_work = a.kv_heads * my_tiles * ((my_chunks + chunks - 1) / chunks);
+            if (sum_of_lanes(my_work) <= (int)gridDim.x || !__any(my_chunks > chunks)) break;
+        }
         upto = my_work;
         for (int d = 1; d < 64; d <<= 1) {
             const int o = __shfl_up(upto, d);
             if (lane >= d) upto += o;
         }
+        if (blockIdx.x == 0 && threadIdx.x == 0) *chunks_of(a, p) = chunks;
     }
     const int n_items = listed ? __builtin_amdgcn_readlane(upto, 63) : gridDim.x;
     for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
@@ -192,10 +208,10 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
         split = id % p.splits;
         b = id / p.splits;
     }
-    TreeKeys<T> keys(a, b, hk, 0);
+    TreeKeys<T> keys(a, b, hk);
     const int n_rows = keys.drafts * group, row0 = tile * 16 * NT;
     const int cached_chunks = (keys.cached + kChunk - 1) / kChunk, n_chunks = cached_chunks + (keys.drafts + kChunk - 1) / kChunk;
-    const int first = split * p.chunks, last = min(n_chunks, first + p.chunks);
+    const int first = split * chunks, last = min(n_chunks, first + chunks);
     if (row0 >= n_rows || first >= last) break;                    // (not listed: the only item)
     keys.pad = cached_chunks * kChunk;
 
@@ -460,8 +476,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
     Fixed<char> kernel_arguments = (Fixed<char>)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(kernel_arguments));
     const AttnTreeArgs &late = *(const AttnTreeArgs *)kernel_arguments;
-    TreeKeys<T> rest(late, b, hk, 0);
-    rest.pad = keys.pad;
+    const TreeKeys<T> rest(late, keys);
 
     // the waves join: each row's maximum and sum, then 16 rows' outputs at a time
     for (int n = 0; n < NT; ++n) {
@@ -484,7 +499,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
         joined[1][threadIdx.x] = sum;
     }
     __syncthreads();
-    const bool whole = n_chunks <= p.chunks;
+    const bool whole = n_chunks <= chunks;
     float *red = (float *)v_even;
     constexpr int ROW = DP + 4;
     for (int n = 0; n < NT; ++n) {
@@ -538,10 +553,11 @@ __global__ __launch_bounds__(256) void attn_tree_join(AttnTreeArgs a, TreePlan p
     typedef typename T::elem E;
     const int lane = threadIdx.x & 63, h = blockIdx.x * 4 + (threadIdx.x >> 6), t = blockIdx.y, b = blockIdx.z;
     if (h >= a.q_heads) return;
-    const TreeKeys<T> keys(a, b, 0, 0);
+    const TreeKeys<T> keys(a, b, 0);
     const int n_chunks = (keys.cached + kChunk - 1) / kChunk + (keys.drafts + kChunk - 1) / kChunk;
-    if (t >= keys.drafts || n_chunks <= p.chunks) return;
-    const int n = (n_chunks + p.chunks - 1) / p.chunks;
+    const int chunks = p.listed ? *chunks_of(a, p) : p.chunks;
+    if (t >= keys.drafts || n_chunks <= chunks) return;
+    const int n = (n_chunks + chunks - 1) / chunks;
     const int64_t first = part_of(a, p, keys.from + t, h, 0);
     const float *stats = stats_of(a, p) + 2 * first, *part = a.partial + first * a.head_dim;
     float top = -INFINITY, sum = 0;
@@ -621,7 +637,7 @@ hawq_status launch(const AttnTreeArgs &a, hipStream_t s) {
 
 size_t attn_tree_workspace(const AttnTreeArgs &a) {
     const TreePlan p = tree_plan(a);
-    return p.splits > 1 ? (size_t)a.total * a.q_heads * p.splits * (a.head_dim + 2) * sizeof(float) : 0;
+    return p.splits > 1 ? (size_t)a.total * a.q_heads * p.splits * (a.head_dim + 2) * sizeof(float) + 16 : 0;
 }
 
 hawq_status launch_attn_tree(const AttnTreeArgs &a, hipStream_t s) { return a.dtype == HAWQ_F16 ? launch<F16>(a, s) : launch<BF16>(a, s); }
