@@ -159,3 +159,31 @@ def convert_resnet(arch, params, scales, bits=None, image_hw=224, num_classes=10
     pool_b, pool_c = dyadic(np.full(C_last, prev_out / (HW * scales["pool"])))   # Appendix E: 1/(H*W) folded in
     return dict(arch=arch, image_hw=image_hw, num_classes=num_classes, layers=layers, pool_b=pool_b, pool_c=pool_c,
                 fc_scale=fc_scale)
+
+
+def quantize_groups(W, group, zero_points=False):
+    """4-bit weights with a scale for every `group` consecutive inputs of an output, as hawq_linear_w4 takes them.  W [N, K] real,
+    K even, group a multiple of 32.  Symmetric (the scheme of quantize_weights, a group in the place of a channel): codes
+    -7..7, HAWQ_S4.  With zero points: codes and zero points 0..15, HAWQ_U4, the group's range always including 0.
+    Returns (w uint8 [N, K/2], scales float64 [N, groups], zeros uint8 [N, groups] or None); the operator takes the scales in the
+    activations' type."""
+    W = np.asarray(W, dtype=np.float64)
+    N, K = W.shape
+    if K % 2 or group <= 0 or group % 32:
+        raise ValueError("quantize_groups: K must be even and group a positive multiple of 32")
+    groups = -(-K // group)
+    padded = np.zeros((N, groups * group))
+    padded[:, :K] = W
+    g = padded.reshape(N, groups, group)
+    if zero_points:
+        lo, hi = np.minimum(g.min(axis=2), 0.0), np.maximum(g.max(axis=2), 0.0)
+        S = np.where(hi > lo, (hi - lo) / 15.0, 1.0)
+        zeros = np.clip(np.rint(-lo / S), 0, 15)
+        q = np.clip(np.rint(g / S[:, :, None]) + zeros[:, :, None], 0, 15)
+    else:
+        amax = np.abs(g).max(axis=2)
+        S = np.where(amax > 0, 2.0 * amax / 15.0, 1.0)
+        zeros = None
+        q = np.clip(np.rint(g / S[:, :, None]), -W_MAX[4], W_MAX[4])
+    q = q.reshape(N, -1)[:, :K].astype(np.int64) & 15
+    return (q[:, 0::2] | q[:, 1::2] << 4).astype(np.uint8), S, None if zeros is None else zeros.astype(np.uint8)
