@@ -308,6 +308,26 @@ def test_cached_values_that_are_not_numbers_stay_in_their_request(value):
         _tree([50, 70], [3, 2], 4, 2, D, "bf16", change=change)
 
 
+@pytest.mark.parametrize("drafts", [[1, 2], [9, 20]])
+@pytest.mark.parametrize("page", [16, 24])
+def test_values_that_are_not_numbers_in_a_cache_that_is_shared_out(drafts, page):
+    """A part of a long cache with a NaN or an infinity in it: its rows and elements, and only those."""
+    def change(q, k, v, caches, table):
+        caches[1][int(table[0, 100]), 3, 0, 5] = _NAN
+        caches[1][int(table[1, 7]), 2, 1] = float("inf")
+        v[1, 0, 9] = -float("inf")
+    for D in (64, 128):
+        _tree([3000, 4500], drafts, 8, 2, D, "bf16", page=page, change=change)
+
+
+def test_many_requests():
+    r = np.random.default_rng(9)
+    cached = r.integers(0, 700, size=70).tolist()
+    _tree(cached, [1] * 70, 2, 1, 64, "f16", masks="chain")
+    _tree(cached, r.integers(1, 30, size=70).tolist(), 2, 1, 64, "bf16", "s8")
+    _tree((r.integers(0, 3000, size=12)).tolist(), r.integers(1, 20, size=12).tolist(), 32, 4, 64, "bf16")
+
+
 def test_tree_pages_outside_the_cache_are_not_seen():
     for D in (64, 20):
         for cache in ("same", "s8"):
@@ -330,6 +350,7 @@ def test_tree_large_scores():
 def test_tree_offsets_past_32_bits():
     """Pages whose elements lie past 2^31 (and bytes past 2^32)."""
     _tree([70, 33], [3, 1], 8, 8, 128, "bf16", page=16, spare=140000)
+    _tree([70, 33], [3, 1], 8, 8, 128, "f16", page=24, spare=94000)
 
 
 def test_tree_long_cache_is_the_same_on_every_run():

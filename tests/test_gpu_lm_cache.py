@@ -144,5 +144,21 @@ def test_store_rows_at_the_ends_of_the_range():
                 _store(12, 2, D, dtype, cache, 16, skip=0.0, change=change)
 
 
+def test_store_broadcast_rows():
+    """Strides of 0: one row of keys and values for every head and token."""
+    import torch
+    import paper_2011_10680_amd as hawq
+    x = torch.randn((1, 1, 64), device="cuda").half()
+    k = x.expand(10, 3, 64)
+    cache = torch.zeros((2, 8, 3, 64), dtype=torch.float16, device="cuda")
+    cd = hawq.CacheDesc(n_pages=2, page=8, kv_heads=3, head_dim=64, dtype=hawq.F16, page_stride=cache.stride(0), token_stride=cache.stride(1), head_stride=cache.stride(2))
+    d = hawq.CacheStoreDesc(cache=cd, total=10, dtype=hawq.F16, k_token=0, k_head=0, v_token=0, v_head=0)
+    other = torch.zeros_like(cache)
+    hawq.hawq_cache_store(d, k, k, torch.arange(3, 13, device="cuda"), cache, other, None, None)
+    torch.cuda.synchronize()
+    flat = cache.view(16, 3, 64)
+    assert torch.equal(cache, other) and torch.equal(flat[3:13], k) and not flat[:3].any() and not flat[13:].any()
+
+
 def test_store_offsets_past_32_bits():
     _store(100, 8, 128, "bf16", "same", 16, spare=140000)

@@ -61,6 +61,30 @@ def test_outputs(N):
     _run(20, N, 96, 32, "bf16", True, False, y_pad=3, seed=N)
 
 
+@pytest.mark.parametrize("M,N,K", [(3, 40, 20000), (20, 6200, 8320), (40, 12300, 4160), (64, 3100, 160), (50, 200, 1056)])
+def test_more_groups_than_fit_at_once(M, N, K):
+    _run(M, N, K, 32, "bf16", True, False, seed=K)
+    _run(M, N, K, 32, "f16", False, True, seed=K)
+
+
+def test_rows_far_apart():
+    """Rows of x whose offsets leave 32 bits of elements inside a tile."""
+    import torch
+    import paper_2011_10680_amd as hawq
+    stride, M, N, K = 1 << 28, 13, 48, 256
+    x = torch.empty((M - 1) * stride + K, dtype=torch.float16, device="cuda").as_strided((M, K), (stride, 1))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    near = torch.randn((M, K), generator=g, device="cuda").half()
+    x.copy_(near)
+    w = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    s = torch.rand((N, 2), generator=g, device="cuda").half()
+    y, want = torch.empty((2, M, N), dtype=torch.float16, device="cuda")
+    for a, out, step in ((x, y, stride), (near, want, K)):
+        hawq.hawq_linear_w4(hawq.LinearW4Desc(M=M, N=N, K=K, group=128, x_dtype=hawq.F16, w_dtype=hawq.S4, x_stride=step, y_stride=N), a, w, s, None, None, out)
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
 @pytest.mark.parametrize("x_pad,x_at,w_at", [(8, 0, 0), (5, 0, 0), (0, 1, 0), (3, 3, 1), (0, 0, 4), (0, 0, 2), (0, 8, 16)])
 def test_strides_and_alignment(x_pad, x_at, w_at):
     for dtype in ("f16", "bf16"):
