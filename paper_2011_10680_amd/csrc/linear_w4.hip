@@ -228,18 +228,35 @@ hawq_status launch(const LinearW4Args &a, hipStream_t s) {
     return check_launch();
 }
 
-// Tiles: as many outputs to a workgroup as still leave about 200 workgroups, since every workgroup reads all of x; more than 32
-// rows in two halves where that makes up for outputs.  Measured (K = 8192, or 4096 below 8192 outputs; us for 16, 32 and 64 outputs a
-// workgroup): 13 rows of 16384 40 / 27 / 25, 30 rows of 4096 10.7 / 13.2 / 17.9, of 8192 34 / 22 / 29, of 16384 64 / 40 / 30; 64 rows of
-// 8192 67 / 39 / 45, of 16384 134 / 76 / 47; in halves 64 rows of 2048 11.3 / 13.0 (whole 18.9), of 4096 19.5 / 13.9 (whole 19.4).
+// Tiles of a workgroup: a larger one reads x fewer times and has more to do for every 128 weights, and what does not come out even
+// over the 256 compute units waits for its last round.  The times are those of a workgroup alone on its unit (K = 4096, groups of 128,
+// us); times the rounds they order the measured ones right, as for 30 rows of 4096 outputs 13.4 / 10.5 / 14.6 (16, 32, 64 outputs, 16
+// rows) and 13.5 / 18.3 (32, 64 outputs, 32 rows), for 64 rows of 8192 (K = 8192) 81 / 53 / 42, 41 / 31 and 45 (64 outputs, 64 rows).
+struct Tiles { int rt, mt; float us; };
+constexpr Tiles kTiles[] = {{1, 1, 8.0f}, {2, 1, 10.0f}, {4, 1, 14.5f}, {2, 2, 13.5f}, {4, 2, 18.3f}, {4, 4, 27.5f}};
+
+int best_tiles(const LinearW4Args &a) {
+    int best = 0;
+    double least = 0;
+    for (int i = 0; i < 6; ++i) {
+        const Tiles &t = kTiles[i];
+        const int64_t blocks = ((int64_t)a.N + 16 * t.rt - 1) / (16 * t.rt) * (((int64_t)a.M + 16 * t.mt - 1) / (16 * t.mt));
+        const double us = t.us * (double)((blocks + 255) / 256);
+        if (i == 0 || us < least) best = i, least = us;
+    }
+    return best;
+}
+
 template <class T, int PIECES, int ALIGN>
 hawq_status pick_tiles(const LinearW4Args &a, hipStream_t s) {
+    const int best = best_tiles(a);
     if constexpr (ALIGN == 16) {
-        if (a.N >= 64 * 192) return a.M <= 16 ? launch<T, 4, 1, PIECES, ALIGN>(a, s) : a.M <= 32 ? launch<T, 4, 2, PIECES, ALIGN>(a, s) : launch<T, 4, 4, PIECES, ALIGN>(a, s);
-        if (a.N >= 32 * 192) return a.M <= 16 ? launch<T, 2, 1, PIECES, ALIGN>(a, s) : a.M <= 32 ? launch<T, 2, 2, PIECES, ALIGN>(a, s) : launch<T, 2, 4, PIECES, ALIGN>(a, s);
-        if (a.N >= 32 * 96 && a.M > 32) return launch<T, 2, 2, PIECES, ALIGN>(a, s);
+        if (best == 1) return launch<T, 2, 1, PIECES, ALIGN>(a, s);
+        if (best == 2) return launch<T, 4, 1, PIECES, ALIGN>(a, s);
+        if (best == 4) return launch<T, 4, 2, PIECES, ALIGN>(a, s);
+        if (best == 5) return launch<T, 4, 4, PIECES, ALIGN>(a, s);
     }
-    return a.M <= 16 ? launch<T, 1, 1, PIECES, ALIGN>(a, s) : launch<T, 1, 2, PIECES, ALIGN>(a, s);
+    return best >= 3 ? launch<T, 2, 2, PIECES, ALIGN>(a, s) : launch<T, 1, 1, PIECES, ALIGN>(a, s);
 }
 
 template <class T, int ALIGN>
