@@ -57,17 +57,11 @@ __device__ __forceinline__ bool find_tile(const AttnPromptArgs &a, int tile, int
         int f = 0, t = 0;
         if (lane < a.n_seqs) sequence_rows(a.starts, lane, a.total, f, t);
         const int n = (t - f + kRows - 1) / kRows;
-        auto sum = [](int v) {
-            for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-            return __builtin_amdgcn_readfirstlane(v);
-        };
-        int most = n;
-        for (int d = 32; d > 0; d >>= 1) most = max(most, __shfl_xor(most, d));
-        int lo = 0, hi = __builtin_amdgcn_readfirstlane(most);             // tiles at place lo or later: more than `tile`; at hi or later: none
-        if (sum(n) <= tile) return false;
+        int lo = 0, hi = max_of_lanes(n);                                   // tiles at place lo or later: more than `tile`; at hi or later: none
+        if (sum_of_lanes(n) <= tile) return false;
         int past = 0;                                                       // tiles at place lo + 1 or later
         while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1, m = sum(max(n - mid, 0));
+            const int mid = (lo + hi) >> 1, m = sum_of_lanes(max(n - mid, 0));
             if (m > tile) lo = mid; else hi = mid, past = m;
         }
         // of the sequences with a tile at this place, the (tile - past)-th
@@ -84,11 +78,7 @@ __device__ __forceinline__ bool find_tile(const AttnPromptArgs &a, int tile, int
         int f = 0, t = 0;
         if (b0 + lane < a.n_seqs) sequence_rows(a.starts, b0 + lane, a.total, f, t);
         const int n = (t - f + kRows - 1) / kRows;
-        int upto = n;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
-        }
+        const int upto = sum_up_to_lane(n);
         const uint64_t past = __ballot(before + upto > tile);
         if (past) {
             const int l = __builtin_ctzll(past);

@@ -117,10 +117,6 @@ __device__ __forceinline__ int64_t part_of(const AttnTreeArgs &a, const TreePlan
 __device__ __forceinline__ float *stats_of(const AttnTreeArgs &a, const TreePlan &p) { return a.partial + (int64_t)a.total * a.q_heads * p.splits * a.head_dim; }
 // behind them the chunks of a part, where the work is listed
 __device__ __forceinline__ int *chunks_of(const AttnTreeArgs &a, const TreePlan &p) { return (int *)(stats_of(a, p) + (int64_t)a.total * a.q_heads * p.splits * 2); }
-__device__ __forceinline__ int sum_of_lanes(int v) {
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return __builtin_amdgcn_readfirstlane(v);
-}
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
@@ -185,11 +181,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
             my_work = a.kv_heads * my_tiles * ((my_chunks + chunks - 1) / chunks);
             if (sum_of_lanes(my_work) <= (int)gridDim.x || !__any(my_chunks > chunks)) break;
         }
-        upto = my_work;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
-        }
+        upto = sum_up_to_lane(my_work);
         if (blockIdx.x == 0 && threadIdx.x == 0) *chunks_of(a, p) = chunks;
     }
     const int n_items = listed ? __builtin_amdgcn_readlane(upto, 63) : gridDim.x;

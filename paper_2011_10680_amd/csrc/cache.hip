@@ -64,11 +64,7 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
             sum_f += f[i];
             sum_p += take[i];
         }
-        int upto_f = sum_f, upto_p = sum_p;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int x = __shfl_up(upto_f, d), y = __shfl_up(upto_p, d);
-            if (lane >= d) upto_f += x, upto_p += y;
-        }
+        const int upto_f = sum_up_to_lane(sum_f), upto_p = sum_up_to_lane(sum_p);
         if (lane == 63) wave_sum[0][wave] = upto_f, wave_sum[1][wave] = upto_p;
         __syncthreads();
         const int first_token = tokens_before, first_page = pages_before;

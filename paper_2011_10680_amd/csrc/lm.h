@@ -97,6 +97,30 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t scalar_rsrc(const void *p, uin
     return __builtin_amdgcn_make_buffer_rsrc((void *)s, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 
+// Sum of v over the lanes up to this one; over all lanes; the largest of non-negative v.  Moves inside rows of 16 lanes, then of whole
+// rows' ends: none waits for an exchange through LDS.  Every lane of the wave takes part.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int sum_up_to_lane(int v) {
+    v += moved<0x111, 0xf>(v);      // from the lane 1, 2, 4, 8 below, 0 past the row's end
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);      // lane 15 of the row below to rows 1 and 3
+    v += moved<0x143, 0xc>(v);      // lane 31 to rows 2 and 3
+    return v;
+}
+__device__ __forceinline__ int sum_of_lanes(int v) { return __builtin_amdgcn_readlane(sum_up_to_lane(v), 63); }
+__device__ __forceinline__ int max_of_lanes(int v) {
+    v = max(v, moved<0x111, 0xf>(v));
+    v = max(v, moved<0x112, 0xf>(v));
+    v = max(v, moved<0x114, 0xf>(v));
+    v = max(v, moved<0x118, 0xf>(v));
+    v = max(v, moved<0x142, 0xa>(v));
+    v = max(v, moved<0x143, 0xc>(v));
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
 // Pointers that the compiler knows to be global memory (a pointer put together from integers is not known to be), and to data that
 // no kernel in flight writes, so that a load from the same place in every lane is a scalar one.
 template <class X> using Global = const __attribute__((address_space(1))) X *;
