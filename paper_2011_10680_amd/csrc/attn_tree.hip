@@ -460,6 +460,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
                 chunk += W;
                 if (chunk >= end) break;
             }
+            if constexpr (!CODES) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (the chunk loaded once more may land where the drafts and the sums go)
         }
         for (; chunk < last; chunk += W) use_drafts(chunk, ve);
     }
