@@ -1,4 +1,5 @@
 // C interface of the language-model operators: host-side argument validation and dispatch.  Nothing here touches device memory.
+#include <algorithm>
 #include <cmath>
 
 #include "lm.h"
@@ -138,7 +139,7 @@ hawq_status hawq_cache_plan(int32_t n_seqs, int32_t page, int32_t table_stride, 
                             int32_t *counts, void *stream) {
     if (!starts || !counts || (n_seqs > 0 && (!cached || !fresh || (table_stride > 0 && !table))) || (n_free > 0 && !free_pages) || (n_slots > 0 && !slots)) return HAWQ_ERR_NULL;
     if (n_seqs < 0 || page <= 0 || table_stride < 0 || n_free < 0 || n_slots < 0) return HAWQ_ERR_SHAPE;
-    if (n_slots > INT32_MAX) return HAWQ_ERR_UNSUPPORTED;
+    if (n_slots > INT32_MAX || (int64_t)n_seqs * std::max(table_stride, 1) > (1 << 30)) return HAWQ_ERR_UNSUPPORTED;      // (the pages taken are counted in 32 bits)
     if (!at_multiple(4, {cached, fresh, free_pages, table, starts, counts}) || !at_multiple(8, {slots})) return HAWQ_ERR_UNSUPPORTED;
     return launch_cache_plan({n_seqs, page, table_stride, n_free, n_slots, cached, fresh, free_pages, table, starts, slots, counts}, (hipStream_t)stream);
 }

@@ -120,6 +120,13 @@ def test_plan(lib):
     assert call(table=TWO) == UNSUPPORTED and call(slots=ctypes.c_void_p(4100)) == UNSUPPORTED
 
 
+def test_plan_of_more_table_entries_than_it_counts(lib):
+    def call(n, width):
+        return lib.hawq_cache_plan(n, 16, width, 3, 9, P, P, P, P, P, P, P, None)
+    assert call(1 << 16, (1 << 14) + 1) == UNSUPPORTED
+    assert call((1 << 30) + 1, 0) == UNSUPPORTED
+
+
 def test_store(lib):
     import paper_2011_10680_amd as hawq
     base = dict(total=5, dtype=hawq.BF16, k_token=128, k_head=64, v_token=128, v_head=64)
