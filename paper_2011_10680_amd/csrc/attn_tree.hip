@@ -77,6 +77,7 @@ struct TreePlan {
     int32_t waves;             // its waves
     int32_t chunks, splits;    // chunks of 32 keys of a workgroup (listed: at least), workgroups over a request's chunks at most
     FastDiv by_group;          // heads of a group
+    FastDiv by_heads, by_units;   // heads of keys, these times row tiles
     int32_t listed;            // workgroups take what work there is in turn, else one workgroup for all that might be
     int32_t blocks;
 };
@@ -90,6 +91,8 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
     p.rows = rows <= 16 ? 16 : 32;
     p.row_tiles = (int32_t)((rows + p.rows - 1) / p.rows);
     p.by_group = fast_div((uint32_t)group);
+    p.by_heads = fast_div((uint32_t)a.kv_heads);
+    p.by_units = fast_div((uint32_t)(a.kv_heads * p.row_tiles));
     const int64_t most = ((int64_t)a.max_cached + kChunk - 1) / kChunk + (a.max_drafts + kChunk - 1) / kChunk, one = (int64_t)a.n_seqs * a.kv_heads * p.row_tiles;
     // caches of up to 1024 tokens are not shared out (no second launch): a workgroup has eight waves where there are few of them
     p.waves = p.rows == 16 && most <= 33 && one <= 256 ? 8 : 4;
@@ -186,19 +189,24 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
     }
     const int n_items = listed ? __builtin_amdgcn_readlane(upto, 63) : gridDim.x;
     for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
-    int b, hk, tile, split, id = item;
+    // Workgroups go to the eight XCDs in turn.  Eight parts at a time are dealt out so that the heads and row tiles of a part follow one
+    // another on one XCD: they share lines (a token's scales, rows of less than a line, for row tiles all) that only its L2 then fetches.
+    int b = 0, id = item, n_here = gridDim.x, tiles = p.row_tiles;
     if (listed) {
         b = __builtin_ctzll(__ballot(upto > item));
-        id -= __builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(my_work, b);
-        const int tiles = __builtin_amdgcn_readlane(my_tiles, b);
-        hk = id % a.kv_heads; id /= a.kv_heads;
-        tile = id % tiles;
-        split = id / tiles;
-    } else {
-        hk = id % a.kv_heads; id /= a.kv_heads;
-        tile = id % p.row_tiles; id /= p.row_tiles;
-        split = id % p.splits;
-        b = id / p.splits;
+        n_here = __builtin_amdgcn_readlane(my_work, b);
+        id -= __builtin_amdgcn_readlane(upto, b) - n_here;
+        tiles = __builtin_amdgcn_readlane(my_tiles, b);
+    }
+    const int units = a.kv_heads * tiles;
+    auto by_units = [&](int x) { return listed ? x / units : (int)fdiv((uint32_t)x, p.by_units); };
+    const int eights = by_units(id >> 3), in = id - eights * 8 * units;
+    const bool dealt = (eights + 1) * 8 * (int64_t)units <= n_here;
+    int split = dealt ? eights * 8 + (in & 7) : by_units(id);
+    const int unit = dealt ? in >> 3 : id - split * units, tile = (int)fdiv((uint32_t)unit, p.by_heads), hk = unit - tile * a.kv_heads;
+    if (!listed) {
+        b = split / p.splits;
+        split -= b * p.splits;
     }
     TreeKeys<T> keys(a, b, hk);
     const int n_rows = keys.drafts * group, row0 = tile * 16 * NT;
