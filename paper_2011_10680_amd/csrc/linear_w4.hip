@@ -8,10 +8,14 @@
 // The zero point and the 16 leave through the sum of x over the group, which one product with a matrix of ones gives for
 // all outputs.  Group sums and totals are 32-bit; nothing is rounded before the result.
 //
-// Bound by the weights' bytes.  A wave reads 16 bytes per lane (four lanes cover 64 bytes of one output's row), and a 4 x 4
+// Bound by the weights' bytes for some rows (13 of 16384 x 8192, groups of 64 with zero points: 20.8 us, 74 MB at 3.5 TB/s, half of the
+// waves' time waiting), by a launch and one chain of loads for one row of a small layer (1000 x 2048: 4.2 us, of which an empty launch
+// is 2.6), and by the vector pipe beyond 32 rows, where a weight is expanded again for every tile of rows.  A wave reads 16 bytes per lane (four lanes cover 64 bytes of one output's row), and a 4 x 4
 // exchange between its quarters turns the four registers into four operands of 32 consecutive weights each, so that a group
 // of 32 has a matrix instruction of its own.  The waves of a workgroup take every W-th 128 weights of the same outputs and
-// add up in LDS: one output's reduction is shared by the whole workgroup, and few outputs still fill the chip.
+// add up in LDS: one output's reduction is shared by the whole workgroup, and few outputs still fill the chip.  The scales of the
+// workgroup's outputs are brought into LDS first, in rows as they lie (read by each lane where it needs them, two bytes here and there,
+// they took the 13 rows from 25 to 30 us).
 #include "lm.h"
 
 namespace hawq {
@@ -57,6 +61,26 @@ __device__ __forceinline__ void exchange_quarters(v4u &d) {
     const v2u a = __builtin_amdgcn_permlane32_swap(d.x, d.z, false, false), b = __builtin_amdgcn_permlane32_swap(d.y, d.w, false, false);
     const v2u e = __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false), f = __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
     d.x = e.x; d.y = e.y; d.z = f.x; d.w = f.y;
+}
+
+// An output by the formula as it stands, one weight after the other: where x times 31 leaves the range, or x is infinite, the two
+// sums of the fast form are, and their difference says nothing.
+template <class T>
+__device__ __forceinline__ float plain_output(const LinearW4Args &a, int m, int n) {
+    typedef typename T::elem E;
+    const E *x = (const E *)a.x + m * a.x_stride, *s = (const E *)a.scales + (int64_t)n * a.groups;
+    const uint8_t *w = a.w + (int64_t)n * (a.K >> 1);
+    float v = 0;
+    for (int g = 0; g < a.groups; ++g) {
+        const int zero = a.zeros ? a.zeros[(int64_t)n * a.groups + g] : 0, end = (int)min((int64_t)(g + 1) * a.group, (int64_t)a.K);
+        float part = 0;
+        for (int k = g * a.group; k < end; ++k) {
+            const int q = w[k >> 1] >> (4 * (k & 1)) & 15;
+            part = fmaf((float)x[k], (float)((a.zeros || q < 8 ? q : q - 16) - zero), part);
+        }
+        v = fmaf((float)s[g], part, v);
+    }
+    return v;
 }
 
 // RT, MT: 16-output and 16-row tiles of a wave.  PIECES: parts of 128 weights with a scale of their own.  ALIGN: bytes the rows of w
@@ -208,6 +232,7 @@ __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_grou
             float v = 0;
             for (int k = 0; k < waves; ++k) v += red[(k * 16 + m) * kRow + n];
             if (m0 + 16 * i + m < a.M && n0 + n < a.N) {
+                if (!(fabsf(v) < INFINITY)) v = plain_output<T>(a, m0 + 16 * i + m, n0 + n);
                 if (a.bias) v += (float)((const E *)a.bias)[n0 + n];
                 y[(int64_t)(m0 + 16 * i + m) * a.y_stride + n0 + n] = (E)v;
             }

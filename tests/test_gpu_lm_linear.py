@@ -130,3 +130,34 @@ def test_no_rows():
     hawq.hawq_linear_w4(d, t, t, t, None, None, t)
     torch.cuda.synchronize()
     assert (t == 5).all()
+
+
+@pytest.mark.parametrize("M,K,group", [(1, 2048, 128), (13, 1000, 64), (70, 352, 32)])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_values_that_are_not_finite_or_near_the_end_of_the_range(M, K, group, zeros):
+    """Each row holds one value besides zeros: an output is that value times one weight, or NaN where an infinity meets a 0."""
+    import torch
+    import paper_2011_10680_amd as hawq
+    N, groups = 100, -(-K // group)
+    r = np.random.default_rng(M)
+    w = r.integers(0, 256, size=(N, K // 2), dtype=np.uint8)
+    s = torch.from_numpy(r.uniform(0.01, 0.1, size=(N, groups)).astype(np.float32)).to(torch.bfloat16)
+    z = r.integers(0, 16, size=(N, groups), dtype=np.uint8) if zeros else None
+    at = r.integers(0, K, size=M)
+    value = np.array([2e37, np.inf, -2e37, np.nan, -np.inf, 1.0, 0.0])[np.arange(M) % 7] if M > 1 else np.array([2e37])
+    x = np.zeros((M, K), dtype=np.float32)
+    x[np.arange(M), at] = value
+    x = torch.from_numpy(x).to(torch.bfloat16)
+    y = torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    d = hawq.LinearW4Desc(M=M, N=N, K=K, group=group, x_dtype=hawq.BF16, w_dtype=hawq.U4 if zeros else hawq.S4, x_stride=K, y_stride=N)
+    hawq.hawq_linear_w4(d, x.cuda(), torch.from_numpy(w).cuda(), s.cuda(), None if z is None else torch.from_numpy(z).cuda(), None, y)
+    got = y.cpu().double().numpy()
+    weight = ref.unpack(w, z, group)
+    xs = x.double().numpy()
+    with np.errstate(invalid="ignore"):
+        want = np.stack([xs[m, at[m]] * weight[:, at[m]] * s.double().numpy()[:, at[m] // group] for m in range(M)])
+    finite = np.isfinite(want)
+    assert (np.isnan(got) == np.isnan(want)).all()
+    assert (got[np.isinf(want)] == want[np.isinf(want)]).all()
+    # products of 8 significant bits by 5 and a scale of 8 are exact in 32 bits, and so is their difference
+    assert (np.abs(got[finite] - want[finite]) <= (ref.ROUND["bf16"] + 4 * ref.F32) * np.abs(want)[finite]).all()
