@@ -136,31 +136,20 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
     }
 }
 
-// Copies of whole vectors: 16 bytes of k (blockIdx.y = 0) or v, kCopies of them a thread.  Bound by the bytes: 20001 tokens of 8 heads
-// of 128 elements 36 us, 164 MB at 4.5 TB/s (a large copy on this device 5.2).
-constexpr int kCopies = 4;
+// Copies of whole vectors: 16 bytes of k (blockIdx.y = 0) or v a thread.  Bound by the bytes: 20001 tokens of 8 heads of 128 elements
+// 34.9 us, 164 MB at 4.7 TB/s (a large copy on this device 5.2); two vectors a thread 35.5, four 38.7, eight 44.3.
 __global__ __launch_bounds__(256) void cache_copy(CacheStoreArgs a, FastDiv by_piece, FastDiv by_head, uint32_t n) {
-    const int pieces = a.head_dim >> 3;
-    const uint16_t *x = (const uint16_t *)(blockIdx.y ? a.v : a.k);
-    uint16_t *y = (uint16_t *)(blockIdx.y ? a.cache.v : a.cache.k);
-    const int64_t x_token = blockIdx.y ? a.v_token : a.k_token, x_head = blockIdx.y ? a.v_head : a.k_head;
-    v4u d[kCopies];
-    int64_t to[kCopies];
-    for (int i = 0; i < kCopies; ++i) {
-        const uint32_t at = (blockIdx.x * kCopies + i) * 256 + threadIdx.x;
-        to[i] = -1;
-        if (at >= n) continue;
-        const uint32_t row = fdiv(at, by_piece), piece = at - row * pieces, t = fdiv(row, by_head), h = row - t * a.kv_heads;
-        const int64_t slot = a.slots[t];
-        if (slot < 0 || slot >= (int64_t)a.cache.n_pages * a.cache.page) continue;
-        int64_t p;
-        if (slot < INT32_MAX) p = fdiv((uint32_t)slot, a.cache.by_page);
-        else p = slot / a.cache.page;
-        to[i] = p * a.cache.page_stride + (slot - p * a.cache.page) * a.cache.token_stride + h * a.cache.head_stride + piece * 8;
-        d[i] = *(const v4u *)(x + t * x_token + h * x_head + piece * 8);
-    }
-    for (int i = 0; i < kCopies; ++i)
-        if (to[i] >= 0) *(v4u *)(y + to[i]) = d[i];
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x;
+    if (at >= n) return;
+    const uint32_t row = fdiv(at, by_piece), piece = at - row * (uint32_t)(a.head_dim >> 3), t = fdiv(row, by_head), h = row - t * a.kv_heads;
+    const int64_t slot = a.slots[t];
+    if (slot < 0 || slot >= (int64_t)a.cache.n_pages * a.cache.page) return;
+    int64_t p;
+    if (slot < INT32_MAX) p = fdiv((uint32_t)slot, a.cache.by_page);
+    else p = slot / a.cache.page;
+    const uint16_t *x = blockIdx.y ? (const uint16_t *)a.v + t * a.v_token + h * a.v_head : (const uint16_t *)a.k + t * a.k_token + h * a.k_head;
+    uint16_t *y = (uint16_t *)(blockIdx.y ? a.cache.v : a.cache.k) + p * a.cache.page_stride + (slot - p * a.cache.page) * a.cache.token_stride + h * a.cache.head_stride;
+    *(v4u *)(y + piece * 8) = *(const v4u *)(x + piece * 8);
 }
 
 // Codes of whole vectors: a group of 8 to 32 lanes a row, eight elements a lane, the maximum by exchanges inside the group.  37 tokens of 8
@@ -260,7 +249,7 @@ hawq_status launch_cache_store(const CacheStoreArgs &a, hipStream_t s) {
             else cache_codes<BF16><<<grid, 256, 0, s>>>(a, by_head, bits);
         } else {
             const uint32_t n = (uint32_t)(rows * (a.head_dim / 8));
-            cache_copy<<<dim3((n + 256 * kCopies - 1) / (256 * kCopies), 2), 256, 0, s>>>(a, fast_div((uint32_t)a.head_dim / 8), by_head, n);
+            cache_copy<<<dim3((n + 255) / 256, 2), 256, 0, s>>>(a, fast_div((uint32_t)a.head_dim / 8), by_head, n);
         }
         return check_launch();
     }
