@@ -206,11 +206,13 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(AttnPromptArgs a, float by
         const float off = m == -INFINITY ? 0.f : m * by_log2e;
         for (int t = 0; t < 2; ++t) {
             typename T::v8 p[2];
+            float sum = 0;      // (of 16 keys before it meets the total: many small weights one by one would be lost beside a large one)
             for (int e = 0; e < 16; ++e) {
                 const float w = __builtin_amdgcn_exp2f(fmaf(sc[t][e], by_log2e, -off));
-                total += w;
+                sum += w;
                 p[e >> 3][e & 7] = (E)w;
             }
+            total += sum;
             for (int s = 0; s < 2; ++s)
                 for (int d = 0; d < DT; ++d) {
                     typedef short v4s __attribute__((ext_vector_type(4)));

@@ -358,13 +358,15 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
                 for (int d = 0; d < D16; ++d) o[n][d] *= keep;
             }
             const float off = m[n] == -INFINITY ? 0.f : m[n];
+            float sum = 0;      // (of the lane's 8 keys before it meets the total, as in prompt attention)
             for (int t = 0; t < 2; ++t)
                 for (int e = 0; e < 4; ++e) {
                     const float w = __builtin_amdgcn_exp2f(sc[t][n][e] - off);
-                    if constexpr (WEIGHTED) total[n] = fmaf(w, iv[t][e], total[n]);
-                    else total[n] += w;
+                    if constexpr (WEIGHTED) sum = fmaf(w, iv[t][e], sum);
+                    else sum += w;
                     pv[n][4 * t + e] = (E)w;
                 }
+            total[n] += sum;
         }
         for (int d = 0; d < D16; ++d) {
             const char *at = vt + (v_base ^ (d << 5));
