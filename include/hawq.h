@@ -432,8 +432,9 @@ hawq_status hawq_linear_w4(const hawq_linear_w4_desc *desc, const void *x, const
  * starts[n_seqs] = total; rows outside every sequence are not written.  head_dim 1..256, q_heads a multiple of kv_heads.
  * A row's result does not depend on keys and values after it, whatever they hold (infinities and NaN included); a row
  * whose scores are all -infinity gives zeros.  Probabilities may be rounded to T before they meet the values.
- * Values are summed with weights up to 2^8 that are divided out at the end: sums of |v| over the keys have to stay below
- * 2^119 (here and in hawq_attn_tree), beyond it a result may be infinite.
+ * Values are summed with weights up to 2^8 (HAWQ_BF16) or 2^15 (HAWQ_F16, so that a weight of 2^-31 of the largest is still held) that
+ * are divided out at the end: sums of |v| over the keys have to stay below 2^119 or 2^112 (here and in hawq_attn_tree), beyond it
+ * a result may be infinite.
  * head_dim a multiple of 8 up to 128 with 16-byte aligned rows runs on the matrix cores.
  */
 typedef struct {

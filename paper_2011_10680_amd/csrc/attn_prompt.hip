@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(AttnPromptArgs a, float by
             top = fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
         }
         // the weights refer to an earlier maximum until one of the wave's queries has outgrown it by 2^8: powers of two cost no
-        // precision, and most tiles then leave o alone
+        // precision, and most tiles then leave o alone.  They are rounded to T for the product (its operands are of 16 bits), from 2^lift on
         if (__any(top * by_log2e > m * by_log2e + 8.f)) {
             const float next = fmaxf(m, top), keep = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - next) * by_log2e);
             m = next;
@@ -203,12 +203,12 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(AttnPromptArgs a, float by
             for (int t = 0; t < DT; ++t)
                 for (int e = 0; e < 16; ++e) o[t][e] *= keep;
         }
-        const float off = m == -INFINITY ? 0.f : m * by_log2e;
+        const float off = m == -INFINITY ? 0.f : fmaf(-m, by_log2e, T::lift);
         for (int t = 0; t < 2; ++t) {
             typename T::v8 p[2];
             float sum = 0;      // (of 16 keys before it meets the total: many small weights one by one would be lost beside a large one)
             for (int e = 0; e < 16; ++e) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(sc[t][e], by_log2e, -off));
+                const float w = __builtin_amdgcn_exp2f(fmaf(sc[t][e], by_log2e, off));
                 sum += w;
                 p[e >> 3][e & 7] = (E)w;
             }

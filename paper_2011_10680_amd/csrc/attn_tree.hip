@@ -9,7 +9,8 @@
 //
 // An 8-bit cache's codes become 16-bit floats exactly; a key's scale multiplies its score.  A value's scale would drive f16
 // weights below their range, so its logarithm joins the exponent instead: the stored weight is exp2(s + log2 vs - m) with the
-// maximum m taken of that sum, and the sum of weights adds it divided by vs.
+// maximum m taken of that sum, and the sum of weights adds it divided by vs.  (Drafts have no scale: beside one a cached weight is lower by
+// its vs, which the 2^7 that halves begin with make up for.)
 //
 // Bound by the cache's bytes where there are many, by the chain of dependent loads (lengths, table, keys) where there are few.
 // 32 heads on 8 of 128 elements, bf16: 32 requests of one token over 500 to 16384 in 8 bits 132 us with the join, 571 MB of codes and
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
                 total[n] *= keep;
                 for (int d = 0; d < D16; ++d) o[n][d] *= keep;
             }
-            const float off = m[n] == -INFINITY ? 0.f : m[n];
+            const float off = m[n] == -INFINITY ? 0.f : m[n] - T::lift;
             float sum = 0;      // (of the lane's 8 keys before it meets the total, as in prompt attention)
             for (int t = 0; t < 2; ++t)
                 for (int e = 0; e < 4; ++e) {
@@ -531,7 +532,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
             } else {
                 const int64_t at = part_of(late, p, rest.from + t, h, split);
                 *(v4f *)(late.partial + at * late.head_dim + d) = v;
-                if (d == 0) *(float2 *)(stats_of(late, p) + 2 * at) = make_float2(joined[0][16 * n + i], sum);
+                if (d == 0) *(float2 *)(stats_of(late, p) + 2 * at) = make_float2(joined[0][16 * n + i] - T::lift, sum);
             }
         }
         __syncthreads();

@@ -10,12 +10,16 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
-// The activations' type T: its name for the matrix instructions and how a float is rounded to it (nearest even).
+// The activations' type T: its name for the matrix instructions and how a float is rounded to it (nearest even).  lift: softmax weights
+// are held as 2^lift times their own size, and no more than 2^8 times that.  A half goes down to 2^-24 and up to 2^16: with weights from
+// 2^7 on, one that is 2^-31 of the largest is still there (from 1 on those below 2^-25 were lost, a thousandth of a result where 40000
+// keys lay 17 nats below one).  bf16 has a float's range.
 struct F16 {
     typedef _Float16 elem;
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
     typedef _Float16 v4 __attribute__((ext_vector_type(4)));
     typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+    static constexpr float lift = 7.f;
     static __device__ __forceinline__ v4f mfma16(v8 a, v8 b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ v16f mfma32(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
@@ -24,6 +28,7 @@ struct BF16 {
     typedef __bf16 v8 __attribute__((ext_vector_type(8)));
     typedef __bf16 v4 __attribute__((ext_vector_type(4)));
     typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+    static constexpr float lift = 0.f;
     static __device__ __forceinline__ v4f mfma16(v8 a, v8 b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ v16f mfma32(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
