@@ -450,7 +450,7 @@ hawq_status hawq_attn_prompt(const hawq_attn_prompt_desc *desc, const void *q, c
 /*
  * A paged cache of keys and of values, two tensors of one shape and layout: element (page, token, head, i) lies at
  * page * page_stride + token * token_stride + head * head_stride + i.  dtype T, or HAWQ_S8 with scales float32
- * [n_pages, page, kv_heads] (one for each token and head, not negative; value = code * scale).
+ * [n_pages, page, kv_heads] (one for each token and head, not negative; value = code * scale, and a scale of 0 goes with codes of 0).
  */
 typedef struct {
     int32_t n_pages, page;         /* pages, tokens of a page */

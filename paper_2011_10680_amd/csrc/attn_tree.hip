@@ -18,7 +18,7 @@
 // join.  8 heads on one of 64, one token over 611: 8.6 us, three chunks a wave.  (Two chunks on their way instead of one
 // measured 139, 34.5 and 9.9: a wave has few chunks, and what it loads beyond them costs more.)
 //
-// Rows whose result is NaN are computed again by the plain path: 0 times an unseen infinity.
+// Rows whose result is NaN are computed again by the plain path: 0 times an unseen infinity, a value's scale that is not 0 and below 2^-90.
 #include "attn_any.h"
 
 namespace hawq {
@@ -388,9 +388,11 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
             __builtin_amdgcn_wave_barrier();
             for (int t = 0; t < 2; ++t) *(v4f *)kf[t] = *(const v4f *)(vlog + 16 * t + 4 * c);
             __builtin_amdgcn_wave_barrier();
-            const float v = mine ? fmaxf(g.vs, 0x1p-100f) : 1.f;
+            // a row of zeros (scale 0) counts with a scale that leaves its weight in the sum; other scales below that (and NaN) make the rows
+            // that see them NaN, for the plain path
+            const float v = mine ? fmaxf(g.vs, 0x1p-90f) : 1.f;
             if (lane < kChunk) {
-                vlog[lane] = mine && g.vs != g.vs ? g.vs : __builtin_amdgcn_logf(v);
+                vlog[lane] = mine && !(g.vs >= 0x1p-90f || g.vs == 0.f) ? __builtin_nanf("") : __builtin_amdgcn_logf(v);
                 vinv[lane] = 1.f / v;
             }
             // V's codes to LDS as T
