@@ -63,22 +63,21 @@ __device__ __forceinline__ void exchange_quarters(v4u &d) {
     d.x = e.x; d.y = e.y; d.z = f.x; d.w = f.y;
 }
 
-// An output by the formula as it stands, one weight after the other: where x times 31 leaves the range, or x is infinite, the two
-// sums of the fast form are, and their difference says nothing.
+// An output by the formula as it stands, one weight after the other, in 64 bits, whose range no product of three leaves: where x times
+// 31 leaves that of 32 bits, or x or a scale is infinite, the two sums of the fast form do, and their difference says nothing.
 template <class T>
-__device__ __forceinline__ float plain_output(const LinearW4Args &a, int m, int n) {
+__device__ __forceinline__ double plain_output(const LinearW4Args &a, int m, int n) {
     typedef typename T::elem E;
     const E *x = (const E *)a.x + m * a.x_stride, *s = (const E *)a.scales + (int64_t)n * a.groups;
     const uint8_t *w = a.w + (int64_t)n * (a.K >> 1);
-    float v = 0;
+    double v = 0;
     for (int g = 0; g < a.groups; ++g) {
         const int zero = a.zeros ? a.zeros[(int64_t)n * a.groups + g] : 0, end = (int)min((int64_t)(g + 1) * a.group, (int64_t)a.K);
-        float part = 0;
+        const double scale = (double)(float)s[g];
         for (int k = g * a.group; k < end; ++k) {
             const int q = w[k >> 1] >> (4 * (k & 1)) & 15;
-            part = fmaf((float)x[k], (float)((a.zeros || q < 8 ? q : q - 16) - zero), part);
+            v += (double)(float)x[k] * (double)((a.zeros || q < 8 ? q : q - 16) - zero) * scale;
         }
-        v = fmaf((float)s[g], part, v);
     }
     return v;
 }
@@ -232,8 +231,9 @@ __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_grou
             float v = 0;
             for (int k = 0; k < waves; ++k) v += red[(k * 16 + m) * kRow + n];
             if (m0 + 16 * i + m < a.M && n0 + n < a.N) {
-                if (!(fabsf(v) < INFINITY)) v = plain_output<T>(a, m0 + 16 * i + m, n0 + n);
-                if (a.bias) v += (float)((const E *)a.bias)[n0 + n];
+                const float bias = a.bias ? (float)((const E *)a.bias)[n0 + n] : 0.f;
+                if (fabsf(v) < INFINITY) v = a.bias ? v + bias : v;
+                else v = (float)(plain_output<T>(a, m0 + 16 * i + m, n0 + n) + (double)bias);
                 y[(int64_t)(m0 + 16 * i + m) * a.y_stride + n0 + n] = (E)v;
             }
         }
