@@ -1,5 +1,6 @@
 // The paged cache: room for new tokens (block tables, slots) and the store of their keys and values.
 #include "lm.h"
+#include "lm_launch.h"
 
 namespace hawq {
 
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(256) void cache_codes(CacheStoreArgs a, FastDiv by_
 template <class T, bool CODES>
 __global__ __launch_bounds__(256) void cache_store_any(CacheStoreArgs a) {
     typedef typename T::elem E;
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t r = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (r >= (int64_t)a.total * a.kv_heads) return;
     const int t = (int)(r / a.kv_heads), h = (int)(r % a.kv_heads);
@@ -234,28 +235,39 @@ hawq_status launch_cache_plan(const CachePlanArgs &a, hipStream_t s) {
     return check_launch();
 }
 
-hawq_status launch_cache_store(const CacheStoreArgs &a, hipStream_t s) {
+hawq_status launch_cache_store(const CacheStoreArgs &all, hipStream_t s) {
+    CacheStoreArgs a = all;
     const bool codes = a.cache.dtype == HAWQ_S8;
-    const int64_t rows = (int64_t)a.total * a.kv_heads;
     const int64_t reads = a.k_token | a.k_head | a.v_token | a.v_head, writes = a.cache.page_stride | a.cache.token_stride | a.cache.head_stride;
     const uintptr_t from = (uintptr_t)a.k | (uintptr_t)a.v, to = (uintptr_t)a.cache.k | (uintptr_t)a.cache.v;
-    if (a.head_dim % 8 == 0 && (reads | writes) % 8 == 0 && from % 16 == 0 && to % (codes ? 8 : 16) == 0 && rows * 32 < INT32_MAX) {
+    // Whole vectors: as many tokens at a time as have fewer than 2^31 threads at 32 a row (the indices' divisions, and a launch)
+    const int64_t at_once = INT32_MAX / 32 / a.kv_heads;
+    if (a.head_dim % 8 == 0 && (reads | writes) % 8 == 0 && from % 16 == 0 && to % (codes ? 8 : 16) == 0 && at_once > 0) {
         const FastDiv by_head = fast_div((uint32_t)a.kv_heads);
-        if (codes) {
-            int bits = 3;
-            while ((8 << bits) < a.head_dim) ++bits;
-            const dim3 grid((unsigned)(((rows << bits) + 255) / 256), 2);
-            if (a.dtype == HAWQ_F16) cache_codes<F16><<<grid, 256, 0, s>>>(a, by_head, bits);
-            else cache_codes<BF16><<<grid, 256, 0, s>>>(a, by_head, bits);
-        } else {
-            const uint32_t n = (uint32_t)(rows * (a.head_dim / 8));
-            cache_copy<<<dim3((n + 255) / 256, 2), 256, 0, s>>>(a, fast_div((uint32_t)a.head_dim / 8), by_head, n);
+        for (int64_t t = 0; t < all.total; t += at_once) {
+            a.total = (int32_t)(all.total - t < at_once ? all.total - t : at_once);
+            a.k = (const uint16_t *)all.k + t * a.k_token;
+            a.v = (const uint16_t *)all.v + t * a.v_token;
+            a.slots = all.slots + t;
+            const int64_t rows = (int64_t)a.total * a.kv_heads;
+            if (codes) {
+                int bits = 3;
+                while ((8 << bits) < a.head_dim) ++bits;
+                const dim3 grid((unsigned)(((rows << bits) + 255) / 256), 2);
+                if (a.dtype == HAWQ_F16) cache_codes<F16><<<grid, 256, 0, s>>>(a, by_head, bits);
+                else cache_codes<BF16><<<grid, 256, 0, s>>>(a, by_head, bits);
+            } else {
+                const uint32_t n = (uint32_t)(rows * (a.head_dim / 8));
+                cache_copy<<<dim3((n + 255) / 256, 2), 256, 0, s>>>(a, fast_div((uint32_t)a.head_dim / 8), by_head, n);
+            }
+            const hawq_status st = check_launch();
+            if (st != HAWQ_OK) return st;
         }
-        return check_launch();
+        return HAWQ_OK;
     }
-    const int64_t blocks = (rows + 3) / 4;
-    if (blocks > INT32_MAX) return HAWQ_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)blocks, 2);
+    const Grid g = spread(((int64_t)a.total * a.kv_heads + 3) / 4, 1, 256);
+    if (g.x == 0) return HAWQ_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)g.x, 2, (unsigned)g.y);
     if (a.dtype == HAWQ_F16) {
         if (codes) cache_store_any<F16, true><<<grid, 256, 0, s>>>(a);
         else cache_store_any<F16, false><<<grid, 256, 0, s>>>(a);

@@ -1,0 +1,35 @@
+"""The language-model operators on the GPU with more rows than one launch along x holds (2^32 threads)."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("D,cache", [(8, "same"), (8, "s8"), (7, "same"), (7, "s8")])
+def test_store_of_very_many_rows(D, cache):
+    """Rows of 8 elements go in whole vectors, of 7 a wave each; their number (70 million) passes what either had in one launch."""
+    import torch
+    import paper_2011_10680_amd as hawq
+    total, heads, page, s8 = 8750000, 8, 32, cache == "s8"
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x = torch.randint(-127, 128, (total, heads, D), generator=g, device="cuda", dtype=torch.int8)
+    x[:, :, 0] = 127                                                              # (an 8-bit row's scale is 127 * (1 / 127): its codes are its elements)
+    k = x.half()
+    n_pages = -(-total // page)
+    kc, vc = torch.full((2, n_pages, page, heads, D), 5, dtype=torch.int8 if s8 else torch.float16, device="cuda")
+    ks, vs = torch.full((2, n_pages, page, heads), 9.0, device="cuda") if s8 else (None, None)
+    slots = torch.arange(total - 1, -1, -1, device="cuda")
+    slots[::1000] = -1
+    cd = hawq.CacheDesc(n_pages=n_pages, page=page, kv_heads=heads, head_dim=D, dtype=hawq.S8 if s8 else hawq.F16, page_stride=kc.stride(0), token_stride=kc.stride(1),
+                        head_stride=kc.stride(2))
+    d = hawq.CacheStoreDesc(cache=cd, total=total, dtype=hawq.F16, k_token=k.stride(0), k_head=k.stride(1), v_token=k.stride(0), v_head=k.stride(1))
+    hawq.hawq_cache_store(d, k, k, slots, kc, vc, ks, vs)
+    torch.cuda.synchronize()
+    want = x.flip(0)
+    kept = (slots >= 0).flip(0)[:, None, None]
+    for c, f in ((kc, ks), (vc, vs)):
+        c = c.view(-1, heads, D)
+        assert torch.equal(c[:total], torch.where(kept, want, torch.full_like(want, 5)).to(c.dtype)) and bool((c[total:] == 5).all())
+        if s8:
+            f = f.view(-1, heads)
+            one = torch.tensor(127.0, device="cuda") * (torch.tensor(1.0, device="cuda") / 127)
+            assert torch.equal(f[:total], torch.where(kept[:, :, 0], one, torch.tensor(9.0, device="cuda")).expand(total, heads)) and bool((f[total:] == 9).all())
