@@ -19,6 +19,7 @@
 // diagonal inside a tile an eighth more products.  Half as many workgroups of eight waves, three or four tiles in LDS, a score product
 // ahead of the tile before and raised wave priorities measured no faster or slower.
 #include "attn_any.h"
+#include "lm_launch.h"
 
 namespace hawq {
 
@@ -37,7 +38,9 @@ template <class T>
 __global__ __launch_bounds__(64) void attn_prompt_any(AttnPromptArgs a) {
     typedef typename T::elem E;
     __shared__ float q_lds[256];
-    const int row = blockIdx.x, h = blockIdx.y, hk = h / (a.q_heads / a.kv_heads);
+    const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (id >= (int64_t)a.total * a.q_heads) return;
+    const int h = (int)(id / a.total), row = (int)(id - (int64_t)h * a.total), hk = h / (a.q_heads / a.kv_heads);
     int from = 0, to = 0;
     // the sequence that holds the row: the last one that begins at or before it (empty ones in between hold nothing)
     int lo = 0, hi = a.n_seqs - 1;
@@ -110,7 +113,7 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(AttnPromptArgs a, float by
 
     // heads that share keys run on one XCD (workgroups go to the eight in turn), the tiles of all heads side by side
     int h = blockIdx.x % a.q_heads;
-    const int tile = blockIdx.x / a.q_heads;
+    const int tile = blockIdx.x / a.q_heads + blockIdx.y * (gridDim.x / a.q_heads);
     if (a.q_heads % 8 == 0) h = (h & 7) * (a.q_heads / 8) + (h >> 3);
     const int hk = h / (a.q_heads / a.kv_heads);
     int from, to, q0;
@@ -280,18 +283,21 @@ bool matrix_form(const AttnPromptArgs &a) {
 
 template <class T>
 hawq_status launch(const AttnPromptArgs &a, hipStream_t s) {
-    const int64_t tiles = ((int64_t)a.total + kRows - 1) / kRows + a.n_seqs, blocks = tiles * a.q_heads;
-    if (matrix_form(a) && blocks <= INT32_MAX) {
+    const int64_t tiles = ((int64_t)a.total + kRows - 1) / kRows + a.n_seqs;
+    const Grid g = spread(tiles, a.q_heads, 256);
+    if (matrix_form(a) && g.x > 0 && tiles <= INT32_MAX) {
         // q . k times a negative scale is (-q) . k times its magnitude; a scale of 0 is as good as the smallest number
         const float c = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1.2e-38f);
         const uint32_t negate = a.scale < 0 ? 0x80008000u : 0u;
-        if (a.head_dim <= 64) attn_prompt<T, 2><<<(unsigned)blocks, 256, 0, s>>>(a, c, negate);
-        else if (a.head_dim <= 96) attn_prompt<T, 3><<<(unsigned)blocks, 256, 0, s>>>(a, c, negate);
-        else attn_prompt<T, 4><<<(unsigned)blocks, 256, 0, s>>>(a, c, negate);
+        const dim3 grid((unsigned)g.x, (unsigned)g.y);
+        if (a.head_dim <= 64) attn_prompt<T, 2><<<grid, 256, 0, s>>>(a, c, negate);
+        else if (a.head_dim <= 96) attn_prompt<T, 3><<<grid, 256, 0, s>>>(a, c, negate);
+        else attn_prompt<T, 4><<<grid, 256, 0, s>>>(a, c, negate);
         return check_launch();
     }
-    if (a.q_heads > 65535) return HAWQ_ERR_UNSUPPORTED;
-    attn_prompt_any<T><<<dim3((unsigned)a.total, (unsigned)a.q_heads), 64, 0, s>>>(a);
+    const Grid each = spread((int64_t)a.total * a.q_heads, 1, 64);
+    if (each.x == 0) return HAWQ_ERR_UNSUPPORTED;
+    attn_prompt_any<T><<<dim3((unsigned)each.x, (unsigned)each.y), 64, 0, s>>>(a);
     return check_launch();
 }
 

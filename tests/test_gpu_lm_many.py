@@ -33,3 +33,20 @@ def test_store_of_very_many_rows(D, cache):
             f = f.view(-1, heads)
             one = torch.tensor(127.0, device="cuda") * (torch.tensor(1.0, device="cuda") / 127)
             assert torch.equal(f[:total], torch.where(kept[:, :, 0], one, torch.tensor(9.0, device="cuda")).expand(total, heads)) and bool((f[total:] == 9).all())
+
+
+@pytest.mark.parametrize("n,heads,D", [(5000, 4096, 8), (135000, 512, 3)])
+def test_prompts_of_very_many_rows(n, heads, D):
+    """As many prompts of one token as make more than 2^32 threads: each gives its own value back."""
+    import torch
+    import paper_2011_10680_amd as hawq
+    g = torch.Generator(device="cuda").manual_seed(D)
+    q = torch.randn((1, 1, D), generator=g, device="cuda").half()
+    v = torch.randn((n, heads, D), generator=g, device="cuda").half()
+    y = torch.full((n + 1, heads, D), 7.0, dtype=torch.float16, device="cuda")
+    starts = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    d = hawq.AttnPromptDesc(n_seqs=n, total=n, q_heads=heads, kv_heads=heads, head_dim=D, dtype=hawq.F16, scale=1.0, q_token=0, q_head=0, k_token=0, k_head=0,
+                            v_token=v.stride(0), v_head=v.stride(1), y_token=y.stride(0), y_head=y.stride(1))
+    hawq.hawq_attn_prompt(d, q, q, v, starts, y)
+    torch.cuda.synchronize()
+    assert torch.equal(y[:n], v) and bool((y[n] == 7).all())
