@@ -17,6 +17,7 @@
 // workgroup's outputs are brought into LDS first, in rows as they lie (read by each lane where it needs them, two bytes here and there,
 // they took the 13 rows from 25 to 30 us).
 #include "lm.h"
+#include "lm_launch.h"
 
 namespace hawq {
 
@@ -241,16 +242,31 @@ __global__ __launch_bounds__(512) void linear_w4(LinearW4Args a, FastDiv by_grou
 }
 
 template <class T, int RT, int MT, int PIECES, int ALIGN>
-hawq_status launch(const LinearW4Args &a, hipStream_t s) {
+hawq_status launch(const LinearW4Args &all, hipStream_t s) {
+    LinearW4Args a = all;
     const int steps = (a.K + 127) / 128, waves = steps < 8 ? steps : 8;
     const int segment = kScaleBytes / (8 * 16 * RT);
     const size_t scales = (size_t)(a.groups < segment ? a.groups : segment) * 16 * RT * 8, sums = (size_t)waves * 16 * (16 * RT + 4) * 4;
-    const dim3 grid((unsigned)((a.N + 16 * RT - 1) / (16 * RT)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
-    if (grid.y > 65535) return HAWQ_ERR_UNSUPPORTED;
     const size_t lds = scales > sums ? scales : sums;
-    if (a.zeros) linear_w4<T, RT, MT, PIECES, ALIGN, true><<<grid, 64 * waves, lds, s>>>(a, fast_div((uint32_t)a.group));
-    else linear_w4<T, RT, MT, PIECES, ALIGN, false><<<grid, 64 * waves, lds, s>>>(a, fast_div((uint32_t)a.group));
-    return check_launch();
+    // as many outputs and rows at a time as a launch holds (more than millions of either)
+    const int64_t n_most = most_blocks(64 * waves) * (16 * RT), m_most = kMostAlong * (16 * MT);
+    for (int64_t n = 0; n < all.N; n += n_most)
+        for (int64_t m = 0; m < all.M; m += m_most) {
+            a.N = (int32_t)(all.N - n < n_most ? all.N - n : n_most);
+            a.M = (int32_t)(all.M - m < m_most ? all.M - m : m_most);
+            a.x = (const uint16_t *)all.x + m * all.x_stride;
+            a.w = all.w + n * (all.K >> 1);
+            a.scales = (const uint16_t *)all.scales + n * all.groups;
+            a.zeros = all.zeros ? all.zeros + n * all.groups : nullptr;
+            a.bias = all.bias ? (const uint16_t *)all.bias + n : nullptr;
+            a.y = (uint16_t *)all.y + m * all.y_stride + n;
+            const dim3 grid((unsigned)(((int64_t)a.N + 16 * RT - 1) / (16 * RT)), (unsigned)(((int64_t)a.M + 16 * MT - 1) / (16 * MT)));
+            if (a.zeros) linear_w4<T, RT, MT, PIECES, ALIGN, true><<<grid, 64 * waves, lds, s>>>(a, fast_div((uint32_t)a.group));
+            else linear_w4<T, RT, MT, PIECES, ALIGN, false><<<grid, 64 * waves, lds, s>>>(a, fast_div((uint32_t)a.group));
+            const hawq_status st = check_launch();
+            if (st != HAWQ_OK) return st;
+        }
+    return HAWQ_OK;
 }
 
 // Tiles of a workgroup: a larger one reads x fewer times and has more to do for every 128 weights, and what does not come out even

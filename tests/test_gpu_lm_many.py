@@ -50,3 +50,21 @@ def test_prompts_of_very_many_rows(n, heads, D):
     hawq.hawq_attn_prompt(d, q, q, v, starts, y)
     torch.cuda.synchronize()
     assert torch.equal(y[:n], v) and bool((y[n] == 7).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(2200000, 3, 2), (1100000, 1, 32)])
+def test_linear_layers_of_very_many_rows(M, N, K):
+    """More than 65535 tiles of rows.  Codes of 1 and small whole numbers: sums of x times a power of two, exact."""
+    import torch
+    import paper_2011_10680_amd as hawq
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x = torch.randint(-8, 9, (M, K), generator=g, device="cuda", dtype=torch.int8).half()
+    w = torch.full((N, K // 2), 0x11, dtype=torch.uint8, device="cuda")
+    scales = (2.0 ** -torch.arange(N, device="cuda")).half()[:, None].contiguous()
+    bias = torch.arange(N, device="cuda").half()
+    whole = torch.full((M + 1, N), 7.0, dtype=torch.float16, device="cuda")
+    d = hawq.LinearW4Desc(M=M, N=N, K=K, group=32, x_dtype=hawq.F16, w_dtype=hawq.S4, x_stride=K, y_stride=N)
+    hawq.hawq_linear_w4(d, x, w, scales, None, bias, whole)
+    torch.cuda.synchronize()
+    want = (x.float().sum(dim=1, keepdim=True) * scales.float().t() + bias.float()).half()
+    assert torch.equal(whole[:M], want) and bool((whole[M] == 7).all())
