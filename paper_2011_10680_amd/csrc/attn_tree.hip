@@ -20,6 +20,7 @@
 //
 // Rows whose result is NaN are computed again by the plain path: 0 times an unseen infinity, a value's scale that is not 0 and below 2^-90.
 #include "attn_any.h"
+#include "lm_launch.h"
 
 namespace hawq {
 
@@ -107,7 +108,7 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
         p.chunks = (int32_t)most;
         p.splits = 1;
         p.listed = 0;
-        p.blocks = one > INT32_MAX ? 0 : (int32_t)one;
+        p.blocks = one > most_blocks(64 * p.waves) ? 0 : (int32_t)one;      // (0: more than a launch holds)
         return p;
     }
     // At least two chunks for a wave.  With 32 rows and up to 64 requests the kernel itself sizes the parts; else enough workgroups for
@@ -118,7 +119,8 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
     p.splits = (int32_t)((most + p.chunks - 1) / p.chunks);
     const int64_t all = one * p.splits, resident = 512;
     p.listed = p.rows > 16 && a.n_seqs <= 64 && all > resident && p.splits > 1;
-    p.blocks = p.listed ? (int32_t)resident : all > INT32_MAX ? 0 : (int32_t)all;      // (0: too many)
+    p.blocks = p.listed ? (int32_t)resident : all > most_blocks(64 * p.waves) ? 0 : (int32_t)all;
+    if (p.blocks == 0) p.splits = 1;
     return p;
 }
 

@@ -68,3 +68,28 @@ def test_linear_layers_of_very_many_rows(M, N, K):
     torch.cuda.synchronize()
     want = (x.float().sum(dim=1, keepdim=True) * scales.float().t() + bias.float()).half()
     assert torch.equal(whole[:M], want) and bool((whole[M] == 7).all())
+
+
+def test_tree_of_very_many_requests_and_heads():
+    """65535 requests of 257 heads: more than 2^32 threads of the matrix form.  A token that sees only itself, and a few with a cached one."""
+    import torch
+    import paper_2011_10680_amd as hawq
+    n, heads, D = 65535, 257, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.zeros((1, 1, D), device="cuda").half()
+    v = torch.randn((n, heads, D), generator=g, device="cuda").half()
+    cache = torch.randn((1, 16, heads, D), generator=g, device="cuda").half()
+    cached = torch.zeros(n, dtype=torch.int32, device="cuda")
+    cached[-3:] = 1
+    y = torch.full((n + 1, heads, D), 7.0, dtype=torch.float16, device="cuda")
+    cd = hawq.CacheDesc(n_pages=1, page=16, kv_heads=heads, head_dim=D, dtype=hawq.F16, page_stride=cache.stride(0), token_stride=cache.stride(1), head_stride=cache.stride(2))
+    d = hawq.AttnTreeDesc(cache=cd, n_seqs=n, total=n, max_drafts=1, max_cached=1, q_heads=heads, dtype=hawq.F16, table_stride=1, scale=1.0, q_token=0, q_head=0, k_token=0,
+                          k_head=0, v_token=v.stride(0), v_head=v.stride(1), y_token=y.stride(0), y_head=y.stride(1))
+    assert hawq.hawq_attn_tree_workspace_bytes(d) == 0
+    hawq.hawq_attn_tree(d, q, q, v, torch.arange(n + 1, dtype=torch.int32, device="cuda"), None, cache, cache, None, None, torch.zeros((n, 1), dtype=torch.int32, device="cuda"),
+                        cached, y, None)
+    torch.cuda.synchronize()
+    assert torch.equal(y[:n - 3], v[:n - 3]) and bool((y[n] == 7).all())
+    want = (v[n - 3:].double() + cache[0, 0].double()) / 2
+    # both weights are 1 (scores of 0) and the sum is exact in 32 bits: one rounding to a half
+    assert torch.equal(y[n - 3:n], want.float().half())
