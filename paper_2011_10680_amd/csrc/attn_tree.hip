@@ -88,9 +88,11 @@ struct TreePlan {
     FastDiv by_heads, by_units;   // heads of keys, these times row tiles
     int32_t listed;            // workgroups take what work there is in turn, else one workgroup for all that might be
     int32_t blocks;
+    int64_t parts;             // partial rows there is room for
 };
 
 constexpr int kChunk = 32;
+constexpr int kPartRows = 32;     // of an item, where the work is listed
 
 TreePlan tree_plan(const AttnTreeArgs &a) {
     TreePlan p;
@@ -107,7 +109,7 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
     if (most <= 33 && (p.waves == 8 || one >= 256)) {
         p.chunks = (int32_t)most;
         p.splits = 1;
-        p.listed = 0;
+        p.parts = p.listed = 0;
         p.blocks = one > most_blocks(64 * p.waves) ? 0 : (int32_t)one;      // (0: more than a launch holds)
         return p;
     }
@@ -121,14 +123,16 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
     p.listed = p.rows > 16 && a.n_seqs <= 64 && all > resident && p.splits > 1;
     p.blocks = p.listed ? (int32_t)resident : all > most_blocks(64 * p.waves) ? 0 : (int32_t)all;
     if (p.blocks == 0) p.splits = 1;
+    p.parts = p.splits == 1 ? 0 : p.listed ? resident * kPartRows : (int64_t)a.total * a.q_heads * p.splits;
     return p;
 }
 
-// partial sums: [row][q head][split][head_dim] floats, then [row][q head][split][2]: maximum (powers of two) and sum of weights
-__device__ __forceinline__ int64_t part_of(const AttnTreeArgs &a, const TreePlan &p, int64_t row, int h, int split) { return (row * a.q_heads + h) * p.splits + split; }
-__device__ __forceinline__ float *stats_of(const AttnTreeArgs &a, const TreePlan &p) { return a.partial + (int64_t)a.total * a.q_heads * p.splits * a.head_dim; }
-// behind them the chunks of a part, where the work is listed
-__device__ __forceinline__ int *chunks_of(const AttnTreeArgs &a, const TreePlan &p) { return (int *)(stats_of(a, p) + (int64_t)a.total * a.q_heads * p.splits * 2); }
+// Partial sums: a part of a row is head_dim floats; then for each the maximum (powers of two) and the sum of weights.  Parts lie as
+// [row][q head][split], or, listed, as [item][row of the tile]: wherever a request is shared out there are no more items than workgroups,
+// so that the room does not grow with the rows and lengths there might be.  A request's items: [row tile][key head][split].
+__device__ __forceinline__ float *stats_of(const AttnTreeArgs &a, const TreePlan &p) { return a.partial + p.parts * a.head_dim; }
+// behind them, listed: the chunks of a part, then the first item of every request
+__device__ __forceinline__ int *list_of(const AttnTreeArgs &a, const TreePlan &p) { return (int *)(stats_of(a, p) + p.parts * 2); }
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
@@ -194,7 +198,11 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
             if (sum_of_lanes(my_work) <= (int)gridDim.x || !__any(my_chunks > chunks)) break;
         }
         upto = sum_up_to_lane(my_work);
-        if (blockIdx.x == 0 && threadIdx.x == 0) *chunks_of(a, p) = chunks;
+        if (blockIdx.x == 0 && wave == 0) {
+            int *list = list_of(a, p);
+            if (lane == 0) list[0] = chunks;
+            if (lane < a.n_seqs) list[1 + lane] = upto - my_work;
+        }
     }
     const int n_items = listed ? __builtin_amdgcn_readlane(upto, 63) : gridDim.x;
     for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
@@ -514,6 +522,8 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
     }
     __syncthreads();
     const bool whole = n_chunks <= chunks;
+    const int item_part = listed && !whole ? (item - id + unit * ((n_chunks + chunks - 1) / chunks) + split) * kPartRows : 0;
+    auto part_at = [&](int row, int t, int h) { return listed ? (int64_t)(item_part + row - row0) : ((int64_t)(rest.from + t) * late.q_heads + h) * p.splits + split; };
     float *red = (float *)v_even;
     constexpr int ROW = DP + 4;
     for (int n = 0; n < NT; ++n) {
@@ -534,7 +544,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
                 for (int k = 0; k < 4; ++k) y[k] = (E)(sum == 0.f ? 0.f : v[k] * by);
                 *(typename T::v4 *)(rest.out(t, h) + d) = y;
             } else {
-                const int64_t at = part_of(late, p, rest.from + t, h, split);
+                const int64_t at = part_at(row, t, h);
                 *(v4f *)(late.partial + at * late.head_dim + d) = v;
                 if (d == 0) *(float2 *)(stats_of(late, p) + 2 * at) = make_float2(joined[0][16 * n + i] - T::lift, sum);
             }
@@ -550,7 +560,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
             if (whole) {
                 store_row<T>(s, rest.out(t, h), late.head_dim);
             } else {
-                const int64_t i = part_of(late, p, rest.from + t, h, split);
+                const int64_t i = part_at(row, t, h);
                 for (int k = 0; k < 4; ++k)
                     if (lane + 64 * k < late.head_dim) late.partial[i * late.head_dim + lane + 64 * k] = s.total == 0.f ? 0.f : s.o[k];
                 if (lane < 2) stats_of(late, p)[2 * i + lane] = lane ? s.total : s.m * kLog2e;
@@ -569,27 +579,35 @@ __global__ __launch_bounds__(256) void attn_tree_join(AttnTreeArgs a, TreePlan p
     if (h >= a.q_heads) return;
     const TreeKeys<T> keys(a, b, 0);
     const int n_chunks = (keys.cached + kChunk - 1) / kChunk + (keys.drafts + kChunk - 1) / kChunk;
-    const int chunks = p.listed ? *chunks_of(a, p) : p.chunks;
+    const int *list = list_of(a, p);
+    const int chunks = p.listed ? list[0] : p.chunks;
     if (t >= keys.drafts || n_chunks <= chunks) return;
     const int n = (n_chunks + chunks - 1) / chunks;
-    const int64_t first = part_of(a, p, keys.from + t, h, 0);
+    int64_t first = ((int64_t)(keys.from + t) * a.q_heads + h) * p.splits;      // this row's parts: from here on,
+    int step = 1;                                                               // this far apart
+    if (p.listed) {
+        const int hk = (int)fdiv((uint32_t)h, p.by_group), group = a.q_heads / a.kv_heads, row = t * group + h - hk * group;
+        first = (int64_t)(list[1 + b] + (row / kPartRows * a.kv_heads + hk) * n) * kPartRows + row % kPartRows;
+        step = kPartRows;
+    }
     const float *stats = stats_of(a, p) + 2 * first, *part = a.partial + first * a.head_dim;
     float top = -INFINITY, sum = 0;
     float2 o = make_float2(0, 0);
-    for (int s = lane; s < n; s += 64) top = fmaxf(top, stats[2 * s]);
+    for (int s = lane; s < n; s += 64) top = fmaxf(top, stats[2 * s * step]);
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
     const int two = min(2 * lane, a.head_dim - 2);      // this lane's elements (past the last: the last ones, not stored)
     for (int s0 = 0; s0 < n; s0 += 64) {       // 64 parts' weights, a lane each; then their outputs, the loads of eight in flight
         const int s = s0 + lane;
         float w = 0;
         if (s < n) {
-            w = stats[2 * s] == top ? 1.f : __builtin_amdgcn_exp2f(stats[2 * s] - top);
-            sum += w * stats[2 * s + 1];
+            const float *at = stats + 2 * s * step;
+            w = at[0] == top ? 1.f : __builtin_amdgcn_exp2f(at[0] - top);
+            sum += w * at[1];
         }
         const int here = min(64, n - s0);
         for (int i = 0; i < here; i += 8) {
             float2 x[8];
-            for (int k = 0; k < 8; ++k) x[k] = *(const float2 *)(part + (int64_t)(s0 + min(i + k, here - 1)) * a.head_dim + two);
+            for (int k = 0; k < 8; ++k) x[k] = *(const float2 *)(part + (int64_t)(s0 + min(i + k, here - 1)) * step * a.head_dim + two);
             for (int k = 0; k < 8; ++k) {
                 const float wi = __shfl(w, min(i + k, 63));        // (0 past the last part)
                 if (i + k < here) {
@@ -651,7 +669,7 @@ hawq_status launch(const AttnTreeArgs &a, hipStream_t s) {
 
 size_t attn_tree_workspace(const AttnTreeArgs &a) {
     const TreePlan p = tree_plan(a);
-    return p.splits > 1 ? (size_t)a.total * a.q_heads * p.splits * (a.head_dim + 2) * sizeof(float) + 16 : 0;
+    return p.splits > 1 ? (size_t)p.parts * (a.head_dim + 2) * sizeof(float) + (p.listed ? 65 * sizeof(int) : 0) : 0;
 }
 
 hawq_status launch_attn_tree(const AttnTreeArgs &a, hipStream_t s) { return a.dtype == HAWQ_F16 ? launch<F16>(a, s) : launch<BF16>(a, s); }

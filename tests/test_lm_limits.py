@@ -1,0 +1,34 @@
+"""What the language-model operators ask of a caller and where they end, on the host: workspace sizes and refusals that need no GPU."""
+import ctypes
+
+import pytest
+
+OK, NULL, SHAPE, DTYPE, RANGE, UNSUPPORTED, DEVICE, WORKSPACE = 0, 1, 2, 3, 4, 6, 7, 8
+
+
+@pytest.fixture(scope="module")
+def hawq():
+    import paper_2011_10680_amd as hawq
+    from paper_2011_10680_amd import build
+    if build.is_stale():
+        build.build()
+    hawq.load_library()
+    return hawq
+
+
+def _tree(hawq, n, drafts, cached, q_heads=32, kv_heads=8, D=128, page=16, total=None, s8=False, **kw):
+    cache = dict(n_pages=1 << 20, page=page, kv_heads=kv_heads, head_dim=D, dtype=hawq.S8 if s8 else hawq.BF16, page_stride=page * kv_heads * D, token_stride=kv_heads * D, head_stride=D)
+    base = dict(n_seqs=n, total=n * drafts if total is None else total, max_drafts=drafts, max_cached=cached, q_heads=q_heads, dtype=hawq.BF16, table_stride=-(-cached // page),
+                scale=0.1, q_token=q_heads * D, q_head=D, k_token=kv_heads * D, k_head=D, v_token=kv_heads * D, v_head=D, y_token=q_heads * D, y_head=D)
+    cache.update(kw.pop("cache", {}))
+    base.update(kw)
+    return hawq.AttnTreeDesc(cache=hawq.CacheDesc(**cache), **base)
+
+
+@pytest.mark.parametrize("n", [1, 4, 16, 64])
+@pytest.mark.parametrize("drafts", [8, 16, 24, 64])
+@pytest.mark.parametrize("cached", [2000, 16384, 131072, 1 << 20])
+def test_workspace_of_drafted_trees_does_not_grow_with_the_bounds(hawq, n, drafts, cached):
+    """512 workgroups write parts of 32 rows at most, of head_dim floats and two more each: 8.5 MB at 128 elements, and a list."""
+    for heads in ((32, 8), (64, 8)):
+        assert hawq.hawq_attn_tree_workspace_bytes(_tree(hawq, n, drafts, cached, *heads)) <= 512 * 32 * 130 * 4 + 4096, (n, drafts, cached, heads)
