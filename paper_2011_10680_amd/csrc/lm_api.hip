@@ -20,21 +20,24 @@ const int64_t kMostStride = (int64_t)1 << 40;
 // strides of a tensor that is read: any that keep addresses inside 64 bits, 0 for a broadcast axis
 bool strides_ok(int64_t token, int64_t head) { return token >= 0 && head >= 0 && token <= kMostStride && head <= kMostStride; }
 
+// a number of rows times a stride, up to 2^71
+typedef __int128 Extent;
+
 // strides of a tensor [n][heads][dim] that is written: no two rows overlap, whichever of the two axes is the outer one
 bool rows_apart(int64_t token, int64_t head, int64_t n, int64_t heads, int64_t dim) {
     if (!strides_ok(token, head) || (heads > 1 && head < dim) || (n > 1 && token < dim)) return false;
-    return n <= 1 || heads <= 1 || token >= (heads - 1) * head + dim || head >= (n - 1) * token + dim;
+    return n <= 1 || heads <= 1 || token >= (Extent)(heads - 1) * head + dim || head >= (Extent)(n - 1) * token + dim;
 }
 
 hawq_status check_cache(const hawq_cache_desc &c, int dtype, const void *k, const void *v, const float *ks, const float *vs, bool pointers) {
     if (c.n_pages < 0 || c.page <= 0 || c.kv_heads <= 0 || c.head_dim <= 0 || c.head_dim > 256) return HAWQ_ERR_SHAPE;
     if (c.dtype != dtype && c.dtype != HAWQ_S8) return HAWQ_ERR_DTYPE;
     if (!rows_apart(c.token_stride, c.head_stride, c.page, c.kv_heads, c.head_dim)) return HAWQ_ERR_SHAPE;
-    const int64_t extent = (c.page - 1) * c.token_stride + (c.kv_heads - 1) * c.head_stride + c.head_dim;
+    const Extent tokens = (Extent)(c.page - 1) * c.token_stride + c.head_dim, extent = tokens + (Extent)(c.kv_heads - 1) * c.head_stride;
     if (c.n_pages > 1 && (c.page_stride < c.head_dim || c.page_stride > kMostStride)) return HAWQ_ERR_SHAPE;
     // pages one behind the other (or the page axis inside the heads', each head's pages together)
-    if (c.n_pages > 1 && c.page_stride < extent && !(c.kv_heads > 1 && c.head_stride >= (c.n_pages - 1) * c.page_stride + (c.page - 1) * c.token_stride + c.head_dim &&
-                                                     c.page_stride >= (c.page - 1) * c.token_stride + c.head_dim)) return HAWQ_ERR_SHAPE;
+    if (c.n_pages > 1 && c.page_stride < extent && !(c.kv_heads > 1 && c.head_stride >= (Extent)(c.n_pages - 1) * c.page_stride + tokens && c.page_stride >= tokens))
+        return HAWQ_ERR_SHAPE;
     if (!pointers) return HAWQ_OK;
     if (c.n_pages > 0 && (!k || !v)) return HAWQ_ERR_NULL;
     if (c.dtype == HAWQ_S8) {

@@ -32,3 +32,21 @@ def test_workspace_of_drafted_trees_does_not_grow_with_the_bounds(hawq, n, draft
     """512 workgroups write parts of 32 rows at most, of head_dim floats and two more each: 8.5 MB at 128 elements, and a list."""
     for heads in ((32, 8), (64, 8)):
         assert hawq.hawq_attn_tree_workspace_bytes(_tree(hawq, n, drafts, cached, *heads)) <= 512 * 32 * 130 * 4 + 4096, (n, drafts, cached, heads)
+
+
+P = ctypes.c_void_p(4096)
+
+
+def test_rows_that_overlap_are_refused_whatever_their_extent(hawq):
+    """Numbers of rows times strides that pass 64 bits: token 2 of a head is token 0 of the next."""
+    many, far = (1 << 24) + 1, 1 << 40
+    lib = hawq.load_library()
+    d = hawq.AttnPromptDesc(n_seqs=0, total=1 << 30, q_heads=many, kv_heads=1, head_dim=64, dtype=hawq.BF16, scale=1.0, q_token=0, q_head=0, k_token=0, k_head=0, v_token=0,
+                            v_head=0, y_token=far // 2, y_head=far)
+    assert lib.hawq_attn_prompt(ctypes.byref(d), P, P, P, P, P, None) == SHAPE
+    for want, cache in ((SHAPE, dict(n_pages=2, page=many, kv_heads=1, token_stride=far, head_stride=0, page_stride=far // 2)),
+                        (SHAPE, dict(n_pages=2, page=4, kv_heads=many, token_stride=64, head_stride=far, page_stride=far // 2)),
+                        (OK, dict(n_pages=many, page=4, kv_heads=2, token_stride=64, head_stride=far // 2, page_stride=far))):
+        cd = hawq.CacheDesc(head_dim=64, dtype=hawq.BF16, **cache)
+        d = hawq.CacheStoreDesc(cache=cd, total=0, dtype=hawq.BF16, k_token=0, k_head=0, v_token=0, v_head=0)
+        assert lib.hawq_cache_store(ctypes.byref(d), P, P, P, P, P, None, None, None) == want, cache
