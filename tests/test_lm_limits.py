@@ -45,7 +45,7 @@ def test_rows_that_overlap_are_refused_whatever_their_extent(hawq):
                             v_head=0, y_token=far // 2, y_head=far)
     assert lib.hawq_attn_prompt(ctypes.byref(d), P, P, P, P, P, None) == SHAPE
     for want, cache in ((SHAPE, dict(n_pages=2, page=many, kv_heads=1, token_stride=far, head_stride=0, page_stride=far // 2)),
-                        (SHAPE, dict(n_pages=2, page=4, kv_heads=many, token_stride=64, head_stride=far, page_stride=far // 2)),
+                        (SHAPE, dict(n_pages=3, page=4, kv_heads=many, token_stride=64, head_stride=far, page_stride=far // 2)),
                         (OK, dict(n_pages=many, page=4, kv_heads=2, token_stride=64, head_stride=far // 2, page_stride=far))):
         cd = hawq.CacheDesc(head_dim=64, dtype=hawq.BF16, **cache)
         d = hawq.CacheStoreDesc(cache=cd, total=0, dtype=hawq.BF16, k_token=0, k_head=0, v_token=0, v_head=0)
