@@ -435,7 +435,7 @@ hawq_status hawq_linear_w4(const hawq_linear_w4_desc *desc, const void *x, const
  * Values are summed with weights up to 2^8 (HAWQ_BF16) or 2^15 (HAWQ_F16, so that a weight of 2^-31 of the largest is still held) that
  * are divided out at the end: sums of |v| over the keys have to stay below 2^119 or 2^112 (here and in hawq_attn_tree), beyond it
  * a result may be infinite.
- * head_dim a multiple of 8 up to 128 with 16-byte aligned rows runs on the matrix cores.
+ * head_dim a multiple of 8 up to 128 with 16-byte aligned rows runs on the matrix cores.  Up to 2^31 - 256 rows.
  */
 typedef struct {
     int32_t n_seqs, total;
@@ -468,7 +468,7 @@ typedef struct {
  * as in hawq_attn_prompt; one drafted token per request is ordinary decoding.  The drafts' keys and values need not be in
  * the cache (hawq_cache_store puts the accepted ones there).  max_drafts (1..64) and max_cached bound the requests'
  * numbers of drafts and of cached tokens; what is beyond them, or beyond table_stride pages, is not seen (nor a row beyond
- * them written), nor is a page whose number is outside the cache.  k_scales / v_scales: with a HAWQ_S8 cache only, else NULL.
+ * them written), nor is a page whose number is outside the cache, nor a request's tokens past 2^31 - 320.  k_scales / v_scales: with a HAWQ_S8 cache only, else NULL.
  * Values that a row does not see do not change it, whatever they hold; a row whose scores are all -infinity gives zeros.
  * Probabilities (times the value's scale) may be rounded to T before they meet the values.  workspace: device memory of
  * hawq_attn_tree_workspace_bytes(desc) bytes (0 for an invalid desc), 16-byte aligned, scratch for partial sums where a

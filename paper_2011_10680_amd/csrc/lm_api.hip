@@ -16,6 +16,7 @@ bool at_multiple(int bytes, std::initializer_list<const void *> pointers) {
 }
 
 const int64_t kMostStride = (int64_t)1 << 40;
+const int kMostKeys = INT32_MAX - 255;      // of a row: the kernels count them in 32 bits, whole tiles at a time
 
 // strides of a tensor that is read: any that keep addresses inside 64 bits, 0 for a broadcast axis
 bool strides_ok(int64_t token, int64_t head) { return token >= 0 && head >= 0 && token <= kMostStride && head <= kMostStride; }
@@ -73,6 +74,7 @@ hawq_status tree_args(const hawq_attn_tree_desc *d, AttnTreeArgs &a) {
     // no request sees more cached tokens than its row of the table has room for
     const int64_t room = (int64_t)a.table_stride * d->cache.page;
     if (a.max_cached > room) a.max_cached = (int32_t)room;
+    a.max_cached = std::min(a.max_cached, kMostKeys - 64);
     if (a.cache.n_pages == 0) a.max_cached = 0;
     return HAWQ_OK;
 }
@@ -107,7 +109,7 @@ hawq_status hawq_attn_prompt(const hawq_attn_prompt_desc *d, const void *q, cons
         return HAWQ_ERR_SHAPE;
     if (d->n_seqs == 0 || d->total == 0) return HAWQ_OK;
     if (!q || !k || !v || !starts || !y) return HAWQ_ERR_NULL;
-    if (!at_multiple(2, {q, k, v, y}) || !at_multiple(4, {starts})) return HAWQ_ERR_UNSUPPORTED;
+    if (d->total > kMostKeys || !at_multiple(2, {q, k, v, y}) || !at_multiple(4, {starts})) return HAWQ_ERR_UNSUPPORTED;
     AttnPromptArgs a{q, k, v, starts, y, d->n_seqs, d->total, d->q_heads, d->kv_heads, d->head_dim, d->dtype, d->scale,
                      d->q_token, d->q_head, d->k_token, d->k_head, d->v_token, d->v_head, d->y_token, d->y_head};
     return launch_attn_prompt(a, (hipStream_t)stream);

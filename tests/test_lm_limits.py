@@ -50,3 +50,13 @@ def test_rows_that_overlap_are_refused_whatever_their_extent(hawq):
         cd = hawq.CacheDesc(head_dim=64, dtype=hawq.BF16, **cache)
         d = hawq.CacheStoreDesc(cache=cd, total=0, dtype=hawq.BF16, k_token=0, k_head=0, v_token=0, v_head=0)
         assert lib.hawq_cache_store(ctypes.byref(d), P, P, P, P, P, None, None, None) == want, cache
+
+
+def test_prompts_of_more_rows_than_are_counted_are_refused(hawq):
+    """Positions are counted in 32 bits, 128 rows or 64 keys at a time: past 2^31 - 256 a count would turn negative, and its loop not end."""
+    d = hawq.AttnPromptDesc(n_seqs=1, total=(1 << 31) - 1, q_heads=1, kv_heads=1, head_dim=1, dtype=hawq.BF16, scale=1.0, q_token=1, q_head=1, k_token=1, k_head=1, v_token=1,
+                            v_head=1, y_token=1, y_head=1)
+    lib = hawq.load_library()
+    assert lib.hawq_attn_prompt(ctypes.byref(d), P, P, P, P, P, None) == UNSUPPORTED
+    d.total, d.n_seqs = (1 << 31) - 256, 0
+    assert lib.hawq_attn_prompt(ctypes.byref(d), P, P, P, P, P, None) == OK
