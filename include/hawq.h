@@ -468,7 +468,8 @@ typedef struct {
  * as in hawq_attn_prompt; one drafted token per request is ordinary decoding.  The drafts' keys and values need not be in
  * the cache (hawq_cache_store puts the accepted ones there).  max_drafts (1..64) and max_cached bound the requests'
  * numbers of drafts and of cached tokens; what is beyond them, or beyond table_stride pages, is not seen (nor a row beyond
- * them written), nor is a page whose number is outside the cache, nor a request's tokens past 2^31 - 320.  k_scales / v_scales: with a HAWQ_S8 cache only, else NULL.
+ * them written), nor is a page whose number is outside the cache, nor a request's tokens past 2^31 - 320.  Up to 65535
+ * requests and heads.  k_scales / v_scales: with a HAWQ_S8 cache only, else NULL.
  * Values that a row does not see do not change it, whatever they hold; a row whose scores are all -infinity gives zeros.
  * Probabilities (times the value's scale) may be rounded to T before they meet the values.  workspace: device memory of
  * hawq_attn_tree_workspace_bytes(desc) bytes (0 for an invalid desc), 16-byte aligned, scratch for partial sums where a

@@ -654,7 +654,6 @@ void launch_form(const AttnTreeArgs &a, const TreePlan &p, hipStream_t s) {
 template <class T>
 hawq_status launch(const AttnTreeArgs &a, hipStream_t s) {
     const TreePlan p = tree_plan(a);
-    if (a.n_seqs > 65535 || a.q_heads > 65535) return HAWQ_ERR_UNSUPPORTED;
     if (!matrix_form(a) || p.blocks == 0) {
         attn_tree_any<T><<<dim3((unsigned)a.max_drafts, (unsigned)a.q_heads, (unsigned)a.n_seqs), 64, 0, s>>>(a);
         return check_launch();

@@ -65,6 +65,7 @@ hawq_status tree_args(const hawq_attn_tree_desc *d, AttnTreeArgs &a) {
     if (!strides_ok(d->q_token, d->q_head) || !strides_ok(d->k_token, d->k_head) || !strides_ok(d->v_token, d->v_head) ||
         !rows_apart(d->y_token, d->y_head, d->total, d->q_heads, d->cache.head_dim))
         return HAWQ_ERR_SHAPE;
+    if (d->n_seqs > 65535 || d->q_heads > 65535) return HAWQ_ERR_UNSUPPORTED;      // (a launch's workgroups along y and z)
     a = AttnTreeArgs{};
     a.cache = cache_args(d->cache, nullptr, nullptr, nullptr, nullptr);
     a.n_seqs = d->n_seqs; a.total = d->total; a.max_drafts = d->max_drafts; a.max_cached = d->max_cached; a.q_heads = d->q_heads;

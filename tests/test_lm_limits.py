@@ -60,3 +60,14 @@ def test_prompts_of_more_rows_than_are_counted_are_refused(hawq):
     assert lib.hawq_attn_prompt(ctypes.byref(d), P, P, P, P, P, None) == UNSUPPORTED
     d.total, d.n_seqs = (1 << 31) - 256, 0
     assert lib.hawq_attn_prompt(ctypes.byref(d), P, P, P, P, P, None) == OK
+
+
+def test_trees_of_more_requests_or_heads_than_a_launch_holds(hawq):
+    lib = hawq.load_library()
+    for over in (dict(n=65536, total=0), dict(n=4, total=0, q_heads=65536, kv_heads=8)):
+        d = _tree(hawq, drafts=20, cached=100000, **over)
+        assert hawq.hawq_attn_tree_workspace_bytes(d) == 0
+        assert lib.hawq_attn_tree(ctypes.byref(d), *[P] * 7, None, None, P, P, P, P, 1 << 40, None) == UNSUPPORTED
+    for most in (dict(n=65535, total=0), dict(n=4, total=0, q_heads=65535, kv_heads=5)):
+        d = _tree(hawq, drafts=20, cached=100000, **most)
+        assert lib.hawq_attn_tree(ctypes.byref(d), *[P] * 7, None, None, P, P, P, P, 1 << 40, None) == OK
