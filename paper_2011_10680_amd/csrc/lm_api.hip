@@ -127,7 +127,7 @@ hawq_status hawq_attn_tree(const hawq_attn_tree_desc *d, const void *q, const vo
     AttnTreeArgs a;
     hawq_status st = tree_args(d, a);
     if (st != HAWQ_OK || d->n_seqs == 0 || d->total == 0) return st;
-    if (!q || !k || !v || !starts || !table || !cached || !y) return HAWQ_ERR_NULL;
+    if (!q || !k || !v || !starts || (a.max_cached > 0 && !table) || !cached || !y) return HAWQ_ERR_NULL;      // (an empty table has no address)
     st = check_cache(d->cache, d->dtype, k_cache, v_cache, k_scales, v_scales, true);
     if (st != HAWQ_OK) return st;
     if (!at_multiple(2, {q, k, v, y}) || !at_multiple(4, {starts, table, cached}) || !at_multiple(8, {mask})) return HAWQ_ERR_UNSUPPORTED;
