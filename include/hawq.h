@@ -408,7 +408,7 @@ hawq_status hawq_net_step_cost(const hawq_net *net, int32_t N, int32_t step, dou
  *   y[m,n] = sum_k x[m,k] * (q[n,k] - z[n, k / group]) * s[n, k / group]  (+ bias[n])
  * w [N, K/2] packed as everywhere (element 2i in bits 0..3): HAWQ_S4 with zeros == NULL (z = 0), or HAWQ_U4 with zeros
  * uint8 [N, groups], values 0..15; scales T [N, groups], groups = ceil(K / group); bias T [N] or NULL.
- * x rows x_stride apart, y rows y_stride apart.  K even, group a positive multiple of 32 (the last group may be short).
+ * x rows x_stride (or 0) apart, y rows y_stride apart.  K even, group a positive multiple of 32 (the last group may be short).
  * The weights may be taken as x * (16 + q) less (16 + z) times the sum of x: an error is that of 32-bit sums of |x| * 31 |s|.
  * Infinities and NaN in x or s give what the formula gives.
  * Made for the rows of a decoding step, a few to some tens: the weights are read once for every 16 to 64 rows of x.

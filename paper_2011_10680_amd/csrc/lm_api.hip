@@ -88,7 +88,7 @@ hawq_status hawq_linear_w4(const hawq_linear_w4_desc *d, const void *x, const vo
                            const void *bias, void *y, void *stream) {
     if (!d) return HAWQ_ERR_NULL;
     if (d->M < 0 || d->N <= 0 || d->K <= 0 || (d->K & 1) || d->group <= 0 || d->group % 32 != 0) return HAWQ_ERR_SHAPE;
-    if (d->x_stride < d->K || d->y_stride < d->N) return HAWQ_ERR_SHAPE;
+    if ((d->x_stride < d->K && d->x_stride != 0) || d->y_stride < d->N) return HAWQ_ERR_SHAPE;      // (0: one row for all)
     if (!float16(d->x_dtype) || (d->w_dtype != HAWQ_S4 && d->w_dtype != HAWQ_U4)) return HAWQ_ERR_DTYPE;
     if (d->w_dtype == HAWQ_S4 && zeros) return HAWQ_ERR_DTYPE;
     if (d->M == 0) return HAWQ_OK;      // (an empty tensor has no address)

@@ -80,3 +80,20 @@ def test_infinite_scales_and_a_bias(zeros):
         assert np.isposinf(want[0, 5]) and np.isnan(want[2, 5])
         size = np.where(np.isfinite(want), 2.0 ** 40 * (K + 100) * ref.F32 * 31 * (np.abs(np.where(np.isfinite(xr), xr, 0)).sum(axis=1)[:, None] * 0.1 + 10), 0)
         _compare(got, want, ref.ROUND[dtype], size)
+
+
+@pytest.mark.parametrize("K", [256, 250])
+@pytest.mark.parametrize("M", [1, 5, 40])
+def test_one_row_of_x_for_all(M, K):
+    """A stride of 0: every row of y is the first one's."""
+    import torch
+    import paper_2011_10680_amd as hawq
+    g = torch.Generator(device="cuda").manual_seed(K)
+    x = torch.randn((1, K), generator=g, device="cuda").half()
+    w = torch.randint(0, 256, (70, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    s = torch.rand((70, 4), generator=g, device="cuda").half()
+    y, want = torch.empty((2, M, 70), dtype=torch.float16, device="cuda")
+    for out, rows in ((y, x.expand(M, K)), (want, x.repeat(M, 1))):
+        d = hawq.LinearW4Desc(M=M, N=70, K=K, group=64, x_dtype=hawq.F16, w_dtype=hawq.S4, x_stride=0 if out is y else K, y_stride=70)
+        hawq.hawq_linear_w4(d, rows, w, s, None, None, out)
+    assert torch.equal(y, want)
