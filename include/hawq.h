@@ -499,7 +499,7 @@ hawq_status hawq_attn_tree(const hawq_attn_tree_desc *desc, const void *q, const
  *   slots   int64 [n_slots]: page * tokens-of-a-page + place of every fresh token, packed by starts; -1 for a token
  *           without a page and for entries past the total
  *   counts  int32 [2]: the total of fresh tokens; the pages taken (more than n_free: the list was too short)
- * Totals must stay below 2^31; a table of more than 2^30 entries is refused.  The inputs and the held part of the table
+ * Totals must stay below 2^31 (a request's tokens past its first 2^31 - 1 get no page and no slot); a table of more than 2^30 entries is refused.  The inputs and the held part of the table
  * are not changed, so a call can be repeated.
  */
 hawq_status hawq_cache_plan(int32_t n_seqs, int32_t page, int32_t table_stride, int32_t n_free, int64_t n_slots, const int32_t *cached,

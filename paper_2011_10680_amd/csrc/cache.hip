@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv 
                     }
                     const uint32_t at = (uint32_t)r.held + (uint32_t)(tk - r.token), p = fdiv(at, by_page);
                     place[k] = at - p * (uint32_t)a.page;
-                    if (p >= (uint32_t)a.table_stride) continue;
+                    if (at >= INT32_MAX || p >= (uint32_t)a.table_stride) continue;      // (no request has more tokens than 32 bits count)
                     const int64_t i = (int64_t)r.taken + p - have;
                     if ((int)p < have) from[k] = a.table + (int64_t)(b0 + b) * a.table_stride + p;
                     else if (i < a.n_free) from[k] = a.free_pages + i;
