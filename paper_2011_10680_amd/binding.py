@@ -178,6 +178,16 @@ def _p(t):
     return None if t is None else t.data_ptr()
 
 
+_integers = None
+
+
+def _integer_types():
+    global _integers
+    import torch
+    _integers = torch.int32, torch.int64
+    return _integers
+
+
 _raw_stream = None
 _fast = None      # the native marshalling module once the device and stream queries it uses are known to work; else None
 
@@ -316,8 +326,17 @@ def hawq_attn_tree(desc, q, k, v, starts, mask, k_cache, v_cache, k_scales, v_sc
 
 
 def hawq_cache_plan(cached, fresh, page, free_pages, table, starts, slots, counts, stream=None):
-    """Sizes are taken from the tensors: requests from cached, the table's row from its second axis, free pages and slots from theirs."""
-    _check(load_library().hawq_cache_plan(cached.numel(), page, table.shape[1], free_pages.numel(), slots.numel(), _p(cached), _p(fresh), _p(free_pages), _p(table),
+    """Sizes are taken from the tensors: requests from cached, the table's row from its second axis, free pages and slots from theirs.
+    Rows of a wider table, or tensors of other sizes or types than the interface names, are refused."""
+    n = cached.numel()
+    int32, int64 = _integers or _integer_types()
+    if not (cached.dtype is fresh.dtype is free_pages.dtype is table.dtype is starts.dtype is counts.dtype is int32 and slots.dtype is int64):
+        raise HawqError(3, "hawq_cache_plan")
+    if fresh.numel() != n or table.dim() != 2 or table.shape[0] != n or starts.numel() <= n or counts.numel() < 2 or not (
+            cached.is_contiguous() and fresh.is_contiguous() and free_pages.is_contiguous() and table.is_contiguous() and starts.is_contiguous() and
+            slots.is_contiguous() and counts.is_contiguous()):
+        raise HawqError(2, "hawq_cache_plan")
+    _check(load_library().hawq_cache_plan(n, page, table.shape[1], free_pages.numel(), slots.numel(), _p(cached), _p(fresh), _p(free_pages), _p(table),
                                            _p(starts), _p(slots), _p(counts), _stream(stream)), "hawq_cache_plan")
 
 
