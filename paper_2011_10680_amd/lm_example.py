@@ -76,10 +76,12 @@ class Decoder:
         self.free = torch.arange(c["pages"], dtype=torch.int32, device="cuda")
         self.table = torch.full((n_requests, -(-most // c["page"])), -1, dtype=torch.int32, device="cuda")
         self.cached = torch.zeros(n_requests, dtype=torch.int32, device="cuda")
-        self.most = 0
+        self.lengths = [0] * n_requests                               # the same on the host
 
     def _room(self, fresh):
         """Slots for `fresh[b]` more tokens of every request; their pages leave the free list."""
+        if max(n + f for n, f in zip(self.lengths, fresh)) > self.table.shape[1] * self.config["page"]:
+            raise RuntimeError("a request has outgrown its row of the block table")
         fresh_d = torch.tensor(fresh, dtype=torch.int32, device="cuda")
         starts = torch.empty(self.n + 1, dtype=torch.int32, device="cuda")
         slots, counts = torch.empty(sum(fresh), dtype=torch.int64, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
@@ -89,6 +91,10 @@ class Decoder:
             raise RuntimeError("the cache is full")
         self.free = self.free[taken:].clone()
         return starts, slots, fresh_d
+
+    def _grow(self, fresh, fresh_d):
+        self.cached += fresh_d
+        self.lengths = [n + f for n, f in zip(self.lengths, fresh)]
 
     def _store(self, layer, k, v, slots):
         d = CacheStoreDesc(cache=self.cache_desc, total=k.shape[0], dtype=_HAWQ[self.dtype], **_strides(k=k, v=v))
@@ -118,8 +124,7 @@ class Decoder:
             hawq_attn_prompt(d, q, k, v, starts, y)
             self._store(i, k, v, slots)
         logits = self._forward(torch.tensor([t for p in prompts for t in p], device="cuda"), attend)
-        self.cached += fresh
-        self.most += max(lens)
+        self._grow(lens, fresh)
         return logits
 
     def check(self, drafts, masks):
@@ -131,7 +136,7 @@ class Decoder:
         self.drafted, self.workspace = [], None
 
         def attend(i, q, k, v, y):
-            d = AttnTreeDesc(cache=self.cache_desc, n_seqs=self.n, total=total, max_drafts=max(lens), max_cached=self.most, q_heads=c["q_heads"], dtype=_HAWQ[self.dtype],
+            d = AttnTreeDesc(cache=self.cache_desc, n_seqs=self.n, total=total, max_drafts=max(lens), max_cached=max(self.lengths), q_heads=c["q_heads"], dtype=_HAWQ[self.dtype],
                              table_stride=self.table.shape[1], scale=c["head_dim"] ** -0.5, **_strides(q=q, k=k, v=v, y=y))
             if self.workspace is None:
                 self.workspace = torch.empty(hawq_attn_tree_workspace_bytes(d), dtype=torch.uint8, device="cuda")
@@ -148,8 +153,7 @@ class Decoder:
         at[torch.tensor(rows, device="cuda")] = slots
         for i, (k, v) in enumerate(self.drafted):
             self._store(i, k, v, at)
-        self.cached += fresh
-        self.most += max(len(k) for k in kept)
+        self._grow([len(k) for k in kept], fresh)
 
 
 def _draft(last, memory, width=2, depth=3):
