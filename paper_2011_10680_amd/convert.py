@@ -14,7 +14,7 @@ residual block is rescaled by its own dyadic number S_res / S_out before the int
 """
 import numpy as np
 
-from .binding import hawq_net_layer_info, hawq_net_num_layers
+from .binding import BF16, F16, hawq_net_layer_info, hawq_net_num_layers
 
 ACT_HI = {8: 127, 4: 15}       # largest activation integer per bit width (unsigned, post-ReLU)
 W_MAX = {8: 127, 4: 7}         # largest weight magnitude per bit width (symmetric)
@@ -161,12 +161,32 @@ def convert_resnet(arch, params, scales, bits=None, image_hw=224, num_classes=10
                 fc_scale=fc_scale)
 
 
-def quantize_groups(W, group, zero_points=False):
+def _rounded_scales(S, used, dtype):
+    """S in 64 bits as the values that f16 or bf16 hold: nearest, and not 0 where a group is used."""
+    if dtype == F16:
+        with np.errstate(over="ignore"):
+            S = S.astype(np.float16).astype(np.float64)
+        least = 2.0 ** -24
+    elif dtype == BF16:
+        with np.errstate(over="ignore"):
+            bits = S.astype(np.float32).view(np.uint32).astype(np.uint64)
+        bits += 0x7FFF + (bits >> 16 & 1)
+        S = (bits & 0xFFFF0000).astype(np.uint32).view(np.float32).astype(np.float64)
+        least = 2.0 ** -133
+    else:
+        raise ValueError("quantize_groups: scales are of type F16 or BF16")
+    if not np.isfinite(S).all():
+        raise ValueError("quantize_groups: a scale is beyond the range of its type")
+    return np.where(used, np.maximum(S, least), S)
+
+
+def quantize_groups(W, group, zero_points=False, dtype=None):
     """4-bit weights with a scale for every `group` consecutive inputs of an output, as hawq_linear_w4 takes them.  W [N, K] real,
     K even, group a multiple of 32.  Symmetric (the scheme of quantize_weights, a group in the place of a channel): codes
     -7..7, HAWQ_S4.  With zero points: codes and zero points 0..15, HAWQ_U4, the group's range always including 0.
-    Returns (w uint8 [N, K/2], scales float64 [N, groups], zeros uint8 [N, groups] or None); the operator takes the scales in the
-    activations' type."""
+    dtype: F16 or BF16, the activations' type, in which the operator takes the scales: codes are then those of the scales so rounded
+    (a bf16 scale is off by up to 0.4 %, at code 7 a thirtieth of a step).
+    Returns (w uint8 [N, K/2], scales float64 [N, groups], zeros uint8 [N, groups] or None)."""
     W = np.asarray(W, dtype=np.float64)
     N, K = W.shape
     if K % 2 or group <= 0 or group % 32:
@@ -177,12 +197,18 @@ def quantize_groups(W, group, zero_points=False):
     g = padded.reshape(N, groups, group)
     if zero_points:
         lo, hi = np.minimum(g.min(axis=2), 0.0), np.maximum(g.max(axis=2), 0.0)
-        S = np.where(hi > lo, (hi - lo) / 15.0, 1.0)
+        used = hi > lo
+        S = np.where(used, (hi - lo) / 15.0, 1.0)
+    else:
+        amax = np.abs(g).max(axis=2)
+        used = amax > 0
+        S = np.where(used, 2.0 * amax / 15.0, 1.0)
+    if dtype is not None:
+        S = _rounded_scales(S, used, dtype)
+    if zero_points:
         zeros = np.clip(np.rint(-lo / S), 0, 15)
         q = np.clip(np.rint(g / S[:, :, None]) + zeros[:, :, None], 0, 15)
     else:
-        amax = np.abs(g).max(axis=2)
-        S = np.where(amax > 0, 2.0 * amax / 15.0, 1.0)
         zeros = None
         q = np.clip(np.rint(g / S[:, :, None]), -W_MAX[4], W_MAX[4])
     q = q.reshape(N, -1)[:, :K].astype(np.int64) & 15

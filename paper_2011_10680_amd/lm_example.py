@@ -28,7 +28,7 @@ class Linear:
     """A weight matrix as the framework holds it: nibbles, scales and, where asked for, zero points."""
 
     def __init__(self, weight, group, dtype, zero_points):
-        w, s, z = quantize_groups(weight, group, zero_points)
+        w, s, z = quantize_groups(weight, group, zero_points, _HAWQ[dtype])
         self.N, self.K, self.group, self.dtype = weight.shape[0], weight.shape[1], group, dtype
         self.w, self.scales = torch.from_numpy(w).cuda(), torch.from_numpy(s).to(dtype).cuda()
         self.zeros = None if z is None else torch.from_numpy(z).cuda()
