@@ -328,16 +328,16 @@ def hawq_attn_tree(desc, q, k, v, starts, mask, k_cache, v_cache, k_scales, v_sc
 def hawq_cache_plan(cached, fresh, page, free_pages, table, starts, slots, counts, stream=None):
     """Sizes are taken from the tensors: requests from cached, the table's row from its second axis, free pages and slots from theirs.
     Rows of a wider table, or tensors of other sizes or types than the interface names, are refused."""
-    n = cached.numel()
     int32, int64 = _integers or _integer_types()
     if not (cached.dtype is fresh.dtype is free_pages.dtype is table.dtype is starts.dtype is counts.dtype is int32 and slots.dtype is int64):
         raise HawqError(3, "hawq_cache_plan")
-    if fresh.numel() != n or table.dim() != 2 or table.shape[0] != n or starts.numel() <= n or counts.numel() < 2 or not (
-            cached.is_contiguous() and fresh.is_contiguous() and free_pages.is_contiguous() and table.is_contiguous() and starts.is_contiguous() and
-            slots.is_contiguous() and counts.is_contiguous()):
+    n, shape, n_starts, n_counts = cached.numel(), table.shape, starts.numel(), counts.numel()
+    if (len(shape) != 2 or shape[0] != n or fresh.numel() != n or n_starts <= n or n_counts < 2 or
+            not (table.is_contiguous() and cached.is_contiguous() and fresh.is_contiguous() and free_pages.is_contiguous() and starts.is_contiguous() and
+                 slots.is_contiguous() and counts.is_contiguous())):
         raise HawqError(2, "hawq_cache_plan")
-    _check(load_library().hawq_cache_plan(n, page, table.shape[1], free_pages.numel(), slots.numel(), _p(cached), _p(fresh), _p(free_pages), _p(table),
-                                           _p(starts), _p(slots), _p(counts), _stream(stream)), "hawq_cache_plan")
+    _check(load_library().hawq_cache_plan(n, page, shape[1], free_pages.numel(), slots.numel(), cached.data_ptr(), fresh.data_ptr(), free_pages.data_ptr(), table.data_ptr(),
+                                           starts.data_ptr(), slots.data_ptr(), counts.data_ptr(), _stream(stream)), "hawq_cache_plan")
 
 
 def hawq_cache_store(desc, k, v, slots, k_cache, v_cache, k_scales, v_scales, stream=None):
