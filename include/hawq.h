@@ -473,7 +473,9 @@ typedef struct {
  * Values that a row does not see do not change it, whatever they hold; a row whose scores are all -infinity gives zeros.
  * Probabilities (times the value's scale) may be rounded to T before they meet the values.  workspace: device memory of
  * hawq_attn_tree_workspace_bytes(desc) bytes (0 for an invalid desc), 16-byte aligned, scratch for partial sums where a
- * long cache is shared out to several workgroups.
+ * long cache is shared out to several workgroups.  Where drafts times heads of a group are 16 or fewer the parts are sized by
+ * max_cached, not by the lengths: a bound far above them leaves a long cache to few workgroups (32 requests of one token over
+ * up to 16384 in 8 bits: 132 us with that bound, 189 with twice, 484 with eight times it).
  */
 typedef struct {
     hawq_cache_desc cache;

@@ -13,8 +13,8 @@
 // the plain path, which leaves unseen values out.
 //
 // Bound by the matrix and vector pipes together: an exponential, a maximum and a sum for every 256 operations of a 128-element
-// head.  32 heads on 8 of 128 elements, bf16, prompts of 8192, 5000 and 8001 tokens: 1.22 ms, 1050 TFLOP/s, matrix pipes busy
-// for 0.58 and vector pipes for 0.50 of the time (a large library product of the type reaches 1485); 12 prompts of 1 to 2048
+// head.  32 heads on 8 of 128 elements, bf16, prompts of 8192, 5000 and 8001 tokens: 1.20 ms, 1060 TFLOP/s, matrix pipes busy
+// for 0.57 and vector pipes for 0.50 of the time (a large library product of the type reaches 1485); 12 prompts of 1 to 2048
 // tokens: 193 us, 745 TFLOP/s, where workgroups live for some ten tiles, their start and end cost a fifth, and keys past the
 // diagonal inside a tile an eighth more products.  Half as many workgroups of eight waves, three or four tiles in LDS, a score product
 // ahead of the tile before and raised wave priorities measured no faster or slower.

@@ -14,8 +14,8 @@
 //
 // Bound by the cache's bytes where there are many, by the chain of dependent loads (lengths, table, keys) where there are few.
 // 32 heads on 8 of 128 elements, bf16: 32 requests of one token over 500 to 16384 in 8 bits 132 us with the join, 571 MB of codes and
-// scales at 4.5 TB/s in the kernel itself; 7 requests of 1 to 64 drafts over caches of 0 to 4097 tokens of 16 bits 28.7 us, 5.2 of them the
-// join.  8 heads on one of 64, one token over 611: 8.6 us, three chunks a wave.  (Two chunks on their way instead of one
+// scales at 4.6 TB/s in the kernel itself; the same in 16 bits 216.  7 requests of 1 to 64 drafts over caches of 0 to 4097 tokens of 16 bits 29 us,
+// 5.4 of them the join.  8 heads on one of 64, one token over 611: 8.9 us, three chunks a wave.  (Two chunks on their way instead of one
 // measured 139, 34.5 and 9.9: a wave has few chunks, and what it loads beyond them costs more.)
 //
 // Rows whose result is NaN are computed again by the plain path: 0 times an unseen infinity, a value's scale that is not 0 and below 2^-90.

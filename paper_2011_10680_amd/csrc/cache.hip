@@ -7,7 +7,7 @@ namespace hawq {
 namespace {
 
 constexpr int kThreads = 1024, kEach = 2, kPass = kThreads * kEach;   // requests of a thread and of a pass
-constexpr int kSlots = 4;                                             // slots of a thread under way (eight: 13.8 us for 2000 requests, 6.4 for few tokens; four: 12.0, 5.7)
+constexpr int kSlots = 4;                                             // slots of a thread under way (2000 requests: eight 13.9 us, four 12.0; few tokens alike)
 
 // ceil(n / page) for n < 2^31
 __device__ __forceinline__ int pages_of(int n, int page, FastDiv by_page) {
@@ -34,7 +34,7 @@ __device__ __forceinline__ int holder(const Request *r, int n, int at) {
 // Every workgroup adds up the tokens and pages of all requests (2048 in a pass: two of a thread, then across the waves), so that one
 // launch does without an order among workgroups, and writes its own share of the slots and of the pages taken.  A thread finds
 // its first slot's request by bisection and walks on from there with the request in registers.  Bound by the chain of dependent steps
-// -- lengths, sums, bisection, page numbers, stores: 5 requests 5.0 us, 2000 with a million fresh tokens and two million
+// -- lengths, sums, bisection, page numbers, stores: 5 requests 4.2 us (a pass with the host's call 5.7), 2000 with a million fresh tokens and two million
 // slots 12.0, 16.3 MB written.
 __global__ __launch_bounds__(kThreads) void cache_plan(CachePlanArgs a, FastDiv by_page, int slots_per_block, int pages_per_block) {
     __shared__ __align__(16) Request request[kPass + 1];
