@@ -10,7 +10,7 @@
 // V^T's operand comes from the transposing LDS read, four keys of one element per lane.
 //
 // Masked probabilities are exact zeros, but 0 * infinity in V would not be: a row whose result is NaN is computed again by
-// the plain path, which leaves unseen values out.
+// the plain path, which leaves unseen values out.  So is a row with scores of millions.
 //
 // Bound by the matrix and vector pipes together: an exponential, a maximum and a sum for every 256 operations of a 128-element
 // head.  32 heads on 8 of 128 elements, bf16, prompts of 8192, 5000 and 8001 tokens: 1.20 ms, 1060 TFLOP/s, matrix pipes busy
@@ -113,7 +113,8 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(AttnPromptArgs a, float by
 
     // heads that share keys run on one XCD (workgroups go to the eight in turn), the tiles of all heads side by side
     int h = blockIdx.x % a.q_heads;
-    const int tile = blockIdx.x / a.q_heads + blockIdx.y * (gridDim.x / a.q_heads);
+    int tile = blockIdx.x / a.q_heads;
+    if (blockIdx.y > 0) tile += blockIdx.y * (gridDim.x / a.q_heads);           // (a second division, where there is need of it)
     if (a.q_heads % 8 == 0) h = (h & 7) * (a.q_heads / 8) + (h >> 3);
     const int hk = h / (a.q_heads / a.kv_heads);
     int from, to, q0;
@@ -209,10 +210,10 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(AttnPromptArgs a, float by
         const float off = m == -INFINITY ? 0.f : fmaf(-m, by_log2e, T::lift);
         for (int t = 0; t < 2; ++t) {
             typename T::v8 p[2];
-            float sum = 0;      // (of 16 keys before it meets the total: many small weights one by one would be lost beside a large one)
+            float sum;          // (of 16 keys before it meets the total: many small weights one by one would be lost beside a large one)
             for (int e = 0; e < 16; ++e) {
                 const float w = __builtin_amdgcn_exp2f(fmaf(sc[t][e], by_log2e, off));
-                sum += w;
+                sum = e == 0 ? w : sum + w;
                 p[e >> 3][e & 7] = (E)w;
             }
             total += sum;
@@ -246,7 +247,8 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(AttnPromptArgs a, float by
         total = __uint_as_float(x.x) + __uint_as_float(x.y);
     }
     const float by = 1.f / total;
-    bool bad = false;
+    // (a maximum of millions: its own weight is 2 to the power of what rounding it left out, which may be beyond any float)
+    bool bad = fabsf(m) * by_log2e > 0x1p22f && m > -INFINITY;
     for (int t = 0; t < DT; ++t)
         for (int e = 0; e < 16; ++e) {
             o[t][e] = total == 0.f ? 0.f : o[t][e] * by;
