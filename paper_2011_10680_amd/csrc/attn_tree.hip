@@ -18,7 +18,8 @@
 // 5.4 of them the join.  8 heads on one of 64, one token over 611: 8.9 us, three chunks a wave.  (Two chunks on their way instead of one
 // measured 139, 34.5 and 9.9: a wave has few chunks, and what it loads beyond them costs more.)
 //
-// Rows whose result is NaN are computed again by the plain path: 0 times an unseen infinity, a value's scale that is not 0 and below 2^-90.
+// Rows whose result is NaN are computed again by the plain path: 0 times an unseen infinity, a value's scale that is not 0 and below 2^-90.  So are
+// rows with scores of thousands (millions over 16 bits).
 #include "attn_any.h"
 #include "lm_launch.h"
 
@@ -171,6 +172,9 @@ template <class T, bool CODES, bool WHOLE, int DT, int NT, int W>
 __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan p, float by_log2e, uint32_t negate) {
     typedef typename T::elem E;
     constexpr int PITCH = DT == 2 ? 128 : 256, D16 = 2 * DT, DP = 32 * DT, TILE = kChunk * PITCH, V_LOADS = TILE / 1024;
+    // Maxima (powers of two) beyond which steps of a float are too coarse for what is added to them: a scale's logarithm, which the sum of
+    // weights does not see rounded (at 2^12 by 2^-12), the 2^7 of halves.  Such rows go to the plain path.
+    constexpr float kMostTop = CODES ? 0x1p12f : T::lift > 0 ? 0x1p22f : INFINITY;
     constexpr int RED = 16 * (DP + 4) * 4 > TILE ? 16 * (DP + 4) * 4 : TILE;       // a wave's part of 16 rows, when the waves join
     __shared__ __align__(1024) char v_even[W * RED], v_odd[CODES ? 16 : W * TILE];   // (codes pass through registers: one buffer)
     __shared__ float scales[W][2][kChunk], stat[W][2][16 * NT], joined[2][16 * NT], q_lds[W][256];
@@ -519,6 +523,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
         }
         joined[0][threadIdx.x] = top;
         joined[1][threadIdx.x] = sum;
+        if (fabsf(top) > kMostTop && top > -INFINITY) atomicOr(&bad, 1u << threadIdx.x);
     }
     __syncthreads();
     const bool whole = n_chunks <= chunks;
@@ -554,8 +559,9 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
     // rows with a NaN once more, the plain way
     int nth = 0;
         for (uint32_t left = bad; left; left &= left - 1, ++nth) {
-            if (nth % W != wave) continue;
-            const int row = row0 + __builtin_ctz(left), t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
+            const int row = row0 + __builtin_ctz(left);
+            if (nth % W != wave || row >= n_rows) continue;
+            const int t = (int)fdiv((uint32_t)row, p.by_group), h = hk * group + row - t * group;
             const RowSums s = rest.attend(t, h, first * kChunk, last * kChunk, q_lds[wave]);
             if (whole) {
                 store_row<T>(s, rest.out(t, h), late.head_dim);

@@ -44,3 +44,46 @@ def test_prompts(j, sign, D):
         d = hawq.AttnPromptDesc(n_seqs=1, total=n, q_heads=1, kv_heads=1, head_dim=D, dtype=ht, scale=2.0 ** j, **base._rows(q=q, k=k, v=v, y=y))
         hawq.hawq_attn_prompt(d, q, k, v, torch.tensor([0, n], dtype=torch.int32, device="cuda"), y)
         _check(base._f64(y)[:, 0], 256 * base._f64(k)[:, 0, 0] * 2.0 ** j, base._f64(v)[:, 0], np.tril(np.ones((n, n), bool)), ref.ROUND[dtype])
+
+
+@pytest.mark.parametrize("j", _J)
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("cache", ["same", "s8"])
+@pytest.mark.parametrize("cached,drafts", [(70, 1), (700, 20), (3000, 1), (6000, 40)])
+def test_caches(j, sign, cache, cached, drafts):
+    import torch
+    import paper_2011_10680_amd as hawq
+    D, page, s8 = 64, 16, cache == "s8"
+    n_pages = -(-cached // page)
+    for dtype in ("f16", "bf16"):
+        dt, ht = base._types(dtype)
+        r = np.random.default_rng(j + cached)
+        q = torch.zeros((drafts, 4, D), dtype=dt, device="cuda")
+        q[:, :, 0] = 256
+        k, v = torch.zeros((drafts, 2, D), dtype=dt, device="cuda"), torch.randn((drafts, 2, D), device="cuda").to(dt)
+        k[:, :, 0] = torch.from_numpy(_keys(r, drafts, sign)).to(dt).cuda()[:, None]
+        kn = _keys(r, n_pages * page, sign)
+        shape = (n_pages, page, 2, D)
+        kc = torch.zeros(shape, dtype=torch.int8 if s8 else dt, device="cuda")
+        if s8:
+            kc[..., 0] = torch.from_numpy(np.floor(kn / 2)).to(torch.int8).cuda().view(n_pages, page, 1)
+            vc = torch.randint(-127, 128, shape, device="cuda", dtype=torch.int8)
+            ks, vs = torch.full(shape[:3], 2.0, device="cuda"), torch.full(shape[:3], 2.0 ** -6, device="cuda")
+        else:
+            kc[..., 0] = torch.from_numpy(kn).to(dt).cuda().view(n_pages, page, 1)
+            vc, ks, vs = torch.randn(shape, device="cuda").to(dt), None, None
+        y = torch.full((drafts, 4, D), 7.0, dtype=dt, device="cuda")
+        cd = hawq.CacheDesc(n_pages=n_pages, page=page, kv_heads=2, head_dim=D, dtype=hawq.S8 if s8 else ht, page_stride=kc.stride(0), token_stride=kc.stride(1),
+                            head_stride=kc.stride(2))
+        d = hawq.AttnTreeDesc(cache=cd, n_seqs=1, total=drafts, max_drafts=drafts, max_cached=cached, q_heads=4, dtype=ht, table_stride=n_pages, scale=2.0 ** j,
+                              **base._rows(q=q, k=k, v=v, y=y))
+        ws = torch.empty(max(16, hawq.hawq_attn_tree_workspace_bytes(d)), dtype=torch.uint8, device="cuda")
+        i32 = dict(dtype=torch.int32, device="cuda")
+        hawq.hawq_attn_tree(d, q, k, v, torch.tensor([0, drafts], **i32), None, kc, vc, ks, vs, torch.arange(n_pages, **i32)[None].contiguous(),
+                            torch.tensor([cached], **i32), y, ws)
+        got = base._f64(y)
+        seen = np.concatenate((np.ones((drafts, cached), bool), np.tril(np.ones((drafts, drafts), bool))), axis=1)
+        for h in range(4):
+            keys = np.concatenate((base._f64(kc)[..., h // 2, 0].reshape(-1)[:cached] * (2 if s8 else 1), base._f64(k)[:, h // 2, 0]))
+            values = np.concatenate((base._f64(vc)[:, :, h // 2].reshape(-1, D)[:cached] * (2.0 ** -6 if s8 else 1), base._f64(v)[:, h // 2]))
+            _check(got[:, h], 256 * keys * 2.0 ** j, values, seen, ref.ROUND[dtype])
