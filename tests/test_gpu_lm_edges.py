@@ -212,3 +212,46 @@ def test_prompt_wrong_starts_write_nothing_else(D, starts, sound):
 def test_listed_parts_over_an_8_bit_cache(strict):
     base._tree([1500, 4500, 70], [9, 20, 11], 32, 8, 128, "bf16", "s8")
     base._tree([1500, 4500, 70, 0, 9000], [9, 64, 11, 3, 1], 32, 8, 64, "f16", "s8", page=24)
+
+
+@pytest.mark.parametrize("form", list(_FORMS))
+@pytest.mark.parametrize("cache", ["same", "s8"])
+def test_tree_with_a_bound_far_above_the_lengths(form, cache):
+    lens = _FORMS[form][3]
+    _tree_as_described(form, [0, 9, 29, 40], 45, lens, 100000, 20, cache=cache, width=6300)
+    _tree_as_described(form, [0, 1, 2, 3], 3, lens, 1 << 20, 1, cache=cache, width=1 << 16)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_the_same_bits_on_every_run(dtype):
+    """Prompts of several sequences, drafted trees that are listed and single tokens over shared-out caches: no order of workgroups shows."""
+    import torch
+    import paper_2011_10680_amd as hawq
+    dt, ht = base._types(dtype)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((1700, 32 + 8 + 8, 128), generator=g, device="cuda").to(dt)
+    q, k, v = x[:, :32], x[:, 32:40], x[:, 40:]
+    cache = torch.randn((400, 16, 8, 128), generator=g, device="cuda").to(dt)
+    codes = torch.randint(-127, 128, cache.shape, generator=g, device="cuda", dtype=torch.int8)
+    scales = torch.rand(cache.shape[:3], generator=g, device="cuda") * 0.01
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table, cached = torch.arange(400, **i32).reshape(2, 200).contiguous(), torch.tensor([3000, 1777], **i32)
+    y = torch.empty((1700, 32, 128), dtype=dt, device="cuda")
+    dp = hawq.AttnPromptDesc(n_seqs=3, total=1700, q_heads=32, kv_heads=8, head_dim=128, dtype=ht, scale=0.09, **base._rows(q=q, k=k, v=v, y=y))
+
+    def tree(drafts, kc, s):
+        cd = hawq.CacheDesc(n_pages=400, page=16, kv_heads=8, head_dim=128, dtype=ht if s is None else hawq.S8, page_stride=kc.stride(0), token_stride=kc.stride(1),
+                            head_stride=kc.stride(2))
+        d = hawq.AttnTreeDesc(cache=cd, n_seqs=2, total=2 * drafts, max_drafts=drafts, max_cached=3000, q_heads=32, dtype=ht, table_stride=200, scale=0.09,
+                              **base._rows(q=q, k=k, v=v, y=y))
+        ws = torch.empty(hawq.hawq_attn_tree_workspace_bytes(d), dtype=torch.uint8, device="cuda").fill_(int(torch.randint(0, 256, (1,))))
+        hawq.hawq_attn_tree(d, q, k, v, torch.tensor([0, drafts, 2 * drafts], **i32), None, kc, kc, s, s, table, cached, y, ws)
+    calls = [lambda: hawq.hawq_attn_prompt(dp, q, k, v, torch.tensor([0, 700, 701, 1700], **i32), y)]
+    calls += [lambda n=n, kc=kc, s=s: tree(n, kc, s) for n in (1, 30) for kc, s in ((cache, None), (codes, scales))]
+    for i, call in enumerate(calls):
+        seen = []
+        for _ in range(4):
+            y.fill_(7.0)
+            call()
+            seen.append(y.clone())
+        assert all(torch.equal(seen[0].view(torch.int16), s.view(torch.int16)) for s in seen[1:]), i
