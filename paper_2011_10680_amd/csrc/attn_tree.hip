@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
         }
         float all = (float)a.kv_heads * (float)my_tiles * (float)my_chunks;
         for (int d = 32; d > 0; d >>= 1) all += __shfl_xor(all, d);
-        chunks = max(chunks, __builtin_amdgcn_readfirstlane((int)(all / (float)gridDim.x) / W * W + W));
+        chunks = max(chunks, __builtin_amdgcn_readfirstlane(first_chunks(all, gridDim.x, W)));
         for (;; chunks += (chunks / 8 + W) / W * W) {
             my_work = a.kv_heads * my_tiles * ((my_chunks + chunks - 1) / chunks);
             if (sum_of_lanes(my_work) <= (int)gridDim.x || !__any(my_chunks > chunks)) break;

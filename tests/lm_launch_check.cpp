@@ -25,6 +25,20 @@ int main() {
                 }
     for (int threads : {64, 256, 512})
         if (most_blocks(threads) * threads >= ((int64_t)1 << 32) || (most_blocks(threads) + 1) * threads < ((int64_t)1 << 32)) return 1;
+    // Parts of listed work: requests of up to 2^26 chunks on up to 65535 heads of keys times row tiles.  From the first size on, the items
+    // of 64 requests stay countable, whatever the requests are.
+    for (int waves : {4, 8})
+        for (int64_t tiles = 1; tiles <= 200000; tiles = tiles * 2 + 1)
+            for (int64_t longest = 1; longest <= ((int64_t)1 << 26) + 2; longest = longest * 3 + 1)
+                for (int like = 1; like <= 64; like += 9) {             // so many are as long as the longest, the rest have one chunk
+                    float all = 0;
+                    for (int b = 0; b < 64; ++b) all += (float)tiles * (float)(b < like ? longest : 1);
+                    const int chunks = first_chunks(all, 512, waves);
+                    ++seen;
+                    if (chunks < waves || chunks % waves != 0) return std::printf("%d chunks of %lld\n", chunks, (long long)longest), 1;
+                    const int64_t items = tiles * (like * ((longest + chunks - 1) / chunks) + 64 - like);
+                    if (items > INT32_MAX / 2) return std::printf("%lld items\n", (long long)items), 1;
+                }
     std::printf("%ld\n", seen);
     return 0;
 }
