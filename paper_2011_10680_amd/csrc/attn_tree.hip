@@ -117,6 +117,7 @@ TreePlan tree_plan(const AttnTreeArgs &a) {
     // At least two chunks for a wave.  With 32 rows and up to 64 requests the kernel itself sizes the parts; else enough workgroups for
     // every compute unit some times over, since the requests are of unequal length.
     int64_t chunks = p.rows > 16 && a.n_seqs <= 64 ? 1 : (most * one + 4095) / 4096;
+    if (chunks > most) chunks = most;       // (many requests over long caches: past 32 bits)
     chunks = (chunks + p.waves - 1) / p.waves * p.waves;
     p.chunks = (int32_t)(chunks < 2 * p.waves ? 2 * p.waves : chunks);
     p.splits = (int32_t)((most + p.chunks - 1) / p.chunks);

@@ -71,3 +71,13 @@ def test_trees_of_more_requests_or_heads_than_a_launch_holds(hawq):
     for most in (dict(n=65535, total=0), dict(n=4, total=0, q_heads=65535, kv_heads=5)):
         d = _tree(hawq, drafts=20, cached=100000, **most)
         assert lib.hawq_attn_tree(ctypes.byref(d), *[P] * 7, None, None, P, P, P, P, 1 << 40, None) == OK
+
+
+@pytest.mark.parametrize("n,heads,cached", [(32768, 16, (1 << 30) - 32), (65535, 8, (1 << 31) - 1), (40000, 16, 1 << 30), (65535, 65535, (1 << 31) - 1), (65, 65535, (1 << 31) - 1)])
+@pytest.mark.parametrize("drafts", [1, 64])
+def test_plans_of_many_requests_over_bounds_near_2_to_the_31(hawq, n, heads, cached, drafts):
+    """Parts are as long as the longest cache at most: chunks times requests and heads pass 32 bits (2^32 of them made a division by 0)."""
+    for q_heads in (heads, heads * (65535 // heads)):
+        d = _tree(hawq, n, drafts, cached, q_heads=q_heads, kv_heads=heads, D=8, page=1 << 16, total=0)
+        assert hawq.hawq_attn_tree_workspace_bytes(d) == 0                          # (one part a request)
+        assert hawq.load_library().hawq_attn_tree(ctypes.byref(d), *[P] * 7, None, None, P, P, P, P, 0, None) == OK
