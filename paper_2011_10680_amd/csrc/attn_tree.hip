@@ -557,7 +557,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_tree(AttnTreeArgs a, TreePlan 
         }
         __syncthreads();
     }
-    // rows with a NaN once more, the plain way
+    // rows with a NaN, or scores too large, once more, the plain way
     int nth = 0;
         for (uint32_t left = bad; left; left &= left - 1, ++nth) {
             const int row = row0 + __builtin_ctz(left);
