@@ -7,7 +7,8 @@
  * b / 2^c (one integer multiply, one rounding right shift; no floating point, no integer
  * division), ReLU / clamp, the dyadic residual addition and integer pooling.  Beside it stand
  * the operators of a language model served from 4-bit weights and a paged cache (second half:
- * hawq_linear_w4, hawq_attn_*, hawq_cache_*), which compute in floating point.
+ * hawq_linear_w4, hawq_attn_*, hawq_cache_*, hawq_rotary, hawq_gated_w4, hawq_adapters,
+ * hawq_logits), which compute in floating point.
  *
  * Conventions that hold for every entry point unless stated otherwise
  * -------------------------------------------------------------------
@@ -522,6 +523,105 @@ typedef struct {
 } hawq_cache_store_desc;
 hawq_status hawq_cache_store(const hawq_cache_store_desc *desc, const void *k, const void *v, const int64_t *slots, void *k_cache,
                              void *v_cache, float *k_scales, float *v_scales, void *stream);
+
+/*
+ * Rotary positions: the first rotary_dim elements of every query and key are turned, pair by pair, by an angle that grows with
+ * the token's position:
+ *   yq[t,h,i] = scale * (q[t,h,i] * cos a - q[t,h,j] * sin a),   yq[t,h,j] = scale * (q[t,h,j] * cos a + q[t,h,i] * sin a),
+ *   a = 2 pi * positions[t] * turns[f],   (i, j) = (f, f + rotary_dim / 2) or (2 f, 2 f + 1),   0 <= f < rotary_dim / 2
+ * and yk likewise; elements from rotary_dim on are as they were.  positions: int32 [total], any.  turns: float64 [rotary_dim / 2], the
+ * revolutions per token of every pair (convert.rotary_turns makes them, scaled for long contexts or not); the product with the
+ * position is taken in 64 bits, so that far positions keep their angle.
+ * yq may be q and yk may be k, with the same strides (HAWQ_ERR_SHAPE otherwise); no other overlap.  kv_heads may be 0 (k and yk are
+ * then not looked at), and so may q_heads.  rotary_dim is even, 2..head_dim, head_dim up to 256, each of the
+ * two up to 65535 heads.
+ * rotary_dim a multiple of 16 with 16-byte aligned rows is read in whole vectors.
+ */
+typedef enum { HAWQ_ROTARY_HALVES = 0, HAWQ_ROTARY_PAIRS = 1 } hawq_rotary_layout;
+typedef struct {
+    int32_t total;
+    int32_t q_heads, kv_heads, head_dim;
+    int32_t rotary_dim;
+    int32_t layout;                /* hawq_rotary_layout */
+    int32_t dtype;                 /* T */
+    float scale;                   /* of what is turned; 1: none */
+    int64_t q_token, q_head, k_token, k_head, yq_token, yq_head, yk_token, yk_head;   /* strides */
+} hawq_rotary_desc;
+hawq_status hawq_rotary(const hawq_rotary_desc *desc, const void *q, const void *k, const int32_t *positions, const double *turns,
+                        void *yq, void *yk, void *stream);
+
+/*
+ * The first half of a gated feed-forward block from 4-bit weights: both projections, the activation and their product,
+ *   y[m,n] = act(g) * u,   g = sum_k x[m,k] * W[n,k] (+ bias[n]),   u = sum_k x[m,k] * W[N + n,k] (+ bias[N + n])
+ * W [2 N, K] as in hawq_linear_w4 (codes, zero points, scales and bias of 2 N rows, the gate's first), with the same types, strides,
+ * sizes and accuracy of g and u, which stay in 32 bits; the result is rounded once.  Infinities and NaN give what the formula gives.
+ * act:  HAWQ_SILU g / (1 + exp(-g));  HAWQ_GELU g Phi(g), Phi the normal distribution's;  HAWQ_GELU_TANH its approximation
+ * g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3)));  HAWQ_RELU max(g, 0).
+ * workspace: device memory of hawq_gated_w4_workspace_bytes(desc) bytes (0 for few rows or an invalid desc), 16-byte aligned, scratch.
+ */
+typedef enum { HAWQ_SILU = 0, HAWQ_GELU = 1, HAWQ_GELU_TANH = 2, HAWQ_RELU = 3 } hawq_activation;
+typedef struct {
+    int32_t M, N, K;               /* rows, outputs (W has 2 N rows), inputs */
+    int32_t group;
+    int32_t x_dtype;               /* T: HAWQ_F16 | HAWQ_BF16 */
+    int32_t w_dtype;               /* HAWQ_S4 | HAWQ_U4 */
+    int32_t activation;            /* hawq_activation */
+    int64_t x_stride, y_stride;
+} hawq_gated_w4_desc;
+size_t hawq_gated_w4_workspace_bytes(const hawq_gated_w4_desc *desc);
+hawq_status hawq_gated_w4(const hawq_gated_w4_desc *desc, const void *x, const void *w, const void *scales, const uint8_t *zeros,
+                          const void *bias, void *y, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Low-rank adapters beside a projection that all requests share, another one for each row:
+ *   y[m,n] = base[m,n] + scales[i] * sum_j b[i,n,j] * sum_k a[i,j,k] * x[m,k],   i = adapter[m],   j < ranks[i]
+ * x [M, K], base and y [M, N], a [n_adapters, max_rank, K], b [n_adapters, N, max_rank] of T with the strides given (elements of a_row and
+ * b_row are contiguous; strides of what is read may be 0); adapter int32 [M], ranks int32 [n_adapters] (as 0..max_rank), scales
+ * float32 [n_adapters].  A row whose adapter is not one of 0..n_adapters - 1 (as -1) gets base as it is.  What lies past an adapter's rank
+ * plays no part, whatever it is.  base is what hawq_linear_w4 left, for instance; y may be base, with its stride (HAWQ_ERR_SHAPE
+ * otherwise), no other overlap.  Rows of one adapter share its reading where they lie near one another.
+ * The inner sums are kept in 32 bits (or as two parts of T that hold 15 bits or more); the result is rounded once.
+ * workspace: device memory of hawq_adapters_workspace_bytes(desc) bytes (0 for an invalid desc), 16-byte aligned, scratch.
+ */
+typedef struct {
+    int32_t M, N, K;
+    int32_t n_adapters, max_rank;
+    int32_t dtype;                 /* T */
+    int64_t x_stride, base_stride, y_stride;
+    int64_t a_adapter, a_row, b_adapter, b_row;   /* strides */
+} hawq_adapters_desc;
+size_t hawq_adapters_workspace_bytes(const hawq_adapters_desc *desc);
+hawq_status hawq_adapters(const hawq_adapters_desc *desc, const void *x, const void *a, const void *b, const int32_t *ranks, const float *scales,
+                          const int32_t *adapter, const void *base, void *y, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * What a server does to the logits before it chooses: row t of request b (rows starts[b] .. starts[b+1] - 1; rows outside every request
+ * are not written) holds the logits x[t, 0..vocab-1] of the token behind drafted token t, and for every token v
+ *   l = x[t,v];   if v occurred: l = l > 0 ? l / r : l * r;   if v was written count > 0 times: l = l - frequency * count - presence;
+ *   y[t,v] = l + bias of v,   or -infinity where the row's mask does not allow v, whatever l is
+ * in 32 bits, rounded once.  (r, presence, frequency) = penalties[b], float32 [n_seqs][3].
+ * Tokens that occurred: past[b * past_stride + i], i < past_lens[b] (as far as the row reaches), those from prompt_lens[b] on written by the
+ * model (prompt_lens == NULL: all), and the drafted tokens j of b whose bit j is set in mask[t], as in hawq_attn_tree (mask == NULL: every
+ * drafted token up to and including t), drafts int32 [total], also written by the model.  A token outside the vocabulary plays no part.
+ * starts == NULL: one row per request (total == n_seqs).  drafts == NULL: no drafted token counts.  penalties == NULL: none, past and drafts
+ * are then not looked at; past_stride == 0: no past, past and past_lens are not looked at.
+ * Biases of request b: bias_ids / bias_values [bias_starts[b] .. bias_starts[b+1] - 1], of n_bias in all; an id listed twice has its last value.
+ * Masks: allowed uint32 [n_allowed, allowed_stride], bit v % 32 of word v / 32 set: v is allowed.  allowed_row int32 [total] picks row t's
+ * (a number outside 0..n_allowed - 1, as -1: everything is allowed); allowed_row == NULL: row t's is the t-th, n_allowed >= total.  A mask
+ * may leave a row empty: all of it is -infinity then.  n_bias == 0 and n_allowed == 0: none, their pointers are not looked at.
+ * y may be x, with its stride (HAWQ_ERR_SHAPE otherwise); only what changes is then written.  No other overlap.
+ */
+typedef struct {
+    int32_t n_seqs, total, vocab;
+    int32_t dtype;                 /* T */
+    int32_t past_stride;
+    int32_t n_bias, n_allowed;
+    int64_t allowed_stride;        /* words */
+    int64_t x_stride, y_stride;
+} hawq_logits_desc;
+hawq_status hawq_logits(const hawq_logits_desc *desc, const void *x, const int32_t *past, const int32_t *past_lens, const int32_t *prompt_lens,
+                        const int32_t *starts, const int32_t *drafts, const uint64_t *mask, const float *penalties, const int32_t *bias_starts,
+                        const int32_t *bias_ids, const float *bias_values, const uint32_t *allowed, const int32_t *allowed_row, void *y, void *stream);
 
 /* Measurement hook for tile-shape sweeps: 0 = the built-in heuristic (default), 1..3 = force one of the
  * matrix-core kernel's workgroup tiles (128x128 as four waves, 64x128, 64x64 channels x pixels) for every

@@ -8,5 +8,7 @@ from .binding import (  # noqa: F401
     hawq_net_num_layers, hawq_net_layer_info, hawq_tune_set_tile, hawq_tune_set_split, hawq_tune_set_fusion, hawq_probe_mfma_peak, hawq_conv_blocked_weights_bytes, hawq_conv_block_weights, hawq_noalloc_workspace_limit, hawq_conv_fragment_weights_bytes, hawq_conv_fragment_weights,
     hawq_bottleneck_tail_int, HawqNet, ConvDesc,
     hawq_linear_w4, hawq_attn_prompt, hawq_attn_tree_workspace_bytes, hawq_attn_tree, hawq_cache_plan, hawq_cache_store,
+    hawq_rotary, hawq_gated_w4_workspace_bytes, hawq_gated_w4, hawq_adapters_workspace_bytes, hawq_adapters, hawq_logits,
+    ROTARY_HALVES, ROTARY_PAIRS, SILU, GELU, GELU_TANH, RELU, RotaryDesc, GatedW4Desc, AdaptersDesc, LogitsDesc,
     LinearW4Desc, AttnPromptDesc, CacheDesc, AttnTreeDesc, CacheStoreDesc,
 )

@@ -69,6 +69,28 @@ class CacheStoreDesc(ctypes.Structure):
     _fields_ = [("cache", CacheDesc), ("total", ctypes.c_int32), ("dtype", ctypes.c_int32)] + _ROWS("k", "v")
 
 
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("total", "q_heads", "kv_heads", "head_dim", "rotary_dim", "layout", "dtype")] + [("scale", ctypes.c_float)] + _ROWS("q", "k", "yq", "yk")
+
+
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+SILU, GELU, GELU_TANH, RELU = 0, 1, 2, 3
+
+
+class GatedW4Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("M", "N", "K", "group", "x_dtype", "w_dtype", "activation")] + [("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64)]
+
+
+class AdaptersDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("M", "N", "K", "n_adapters", "max_rank", "dtype")] + [(n, ctypes.c_int64) for n in
+                ("x_stride", "base_stride", "y_stride", "a_adapter", "a_row", "b_adapter", "b_row")]
+
+
+class LogitsDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "total", "vocab", "dtype", "past_stride", "n_bias", "n_allowed")] + [(n, ctypes.c_int64) for n in
+                ("allowed_stride", "x_stride", "y_stride")]
+
+
 _lib = None
 
 
@@ -155,6 +177,18 @@ def load_library():
     lib.hawq_cache_plan.argtypes = [i32] * 4 + [i64] + [vp] * 8
     lib.hawq_cache_store.restype = ctypes.c_int
     lib.hawq_cache_store.argtypes = [ctypes.POINTER(CacheStoreDesc)] + [vp] * 8
+    lib.hawq_rotary.restype = ctypes.c_int
+    lib.hawq_rotary.argtypes = [ctypes.POINTER(RotaryDesc)] + [vp] * 7
+    lib.hawq_gated_w4_workspace_bytes.restype = sz
+    lib.hawq_gated_w4_workspace_bytes.argtypes = [ctypes.POINTER(GatedW4Desc)]
+    lib.hawq_gated_w4.restype = ctypes.c_int
+    lib.hawq_gated_w4.argtypes = [ctypes.POINTER(GatedW4Desc)] + [vp] * 7 + [sz, vp]
+    lib.hawq_adapters_workspace_bytes.restype = sz
+    lib.hawq_adapters_workspace_bytes.argtypes = [ctypes.POINTER(AdaptersDesc)]
+    lib.hawq_adapters.restype = ctypes.c_int
+    lib.hawq_adapters.argtypes = [ctypes.POINTER(AdaptersDesc)] + [vp] * 9 + [sz, vp]
+    lib.hawq_logits.restype = ctypes.c_int
+    lib.hawq_logits.argtypes = [ctypes.POINTER(LogitsDesc)] + [vp] * 15
     lib.hawq_status_string.restype = ctypes.c_char_p
     lib.hawq_status_string.argtypes = [ctypes.c_int]
     _lib = lib
@@ -343,6 +377,40 @@ def hawq_cache_plan(cached, fresh, page, free_pages, table, starts, slots, count
 def hawq_cache_store(desc, k, v, slots, k_cache, v_cache, k_scales, v_scales, stream=None):
     _check(load_library().hawq_cache_store(ctypes.byref(desc), _p(k), _p(v), _p(slots), _p(k_cache), _p(v_cache), _p(k_scales), _p(v_scales), _stream(stream)),
            "hawq_cache_store")
+
+
+def hawq_rotary(desc, q, k, positions, turns, yq, yk, stream=None):
+    _check(load_library().hawq_rotary(ctypes.byref(desc), _p(q), _p(k), _p(positions), _p(turns), _p(yq), _p(yk), _stream(stream)), "hawq_rotary")
+
+
+def _room(workspace):
+    """Bytes of a workspace tensor, None where none is needed."""
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def hawq_gated_w4_workspace_bytes(desc):
+    return int(load_library().hawq_gated_w4_workspace_bytes(ctypes.byref(desc)))
+
+
+def hawq_gated_w4(desc, x, w, scales, zeros, bias, y, workspace=None, stream=None):
+    """workspace: a tensor of at least hawq_gated_w4_workspace_bytes(desc) bytes, or None where that is 0."""
+    _check(load_library().hawq_gated_w4(ctypes.byref(desc), _p(x), _p(w), _p(scales), _p(zeros), _p(bias), _p(y), _p(workspace), _room(workspace), _stream(stream)),
+           "hawq_gated_w4")
+
+
+def hawq_adapters_workspace_bytes(desc):
+    return int(load_library().hawq_adapters_workspace_bytes(ctypes.byref(desc)))
+
+
+def hawq_adapters(desc, x, a, b, ranks, scales, adapter, base, y, workspace, stream=None):
+    """workspace: a tensor of at least hawq_adapters_workspace_bytes(desc) bytes."""
+    _check(load_library().hawq_adapters(ctypes.byref(desc), _p(x), _p(a), _p(b), _p(ranks), _p(scales), _p(adapter), _p(base), _p(y), _p(workspace), _room(workspace),
+                                         _stream(stream)), "hawq_adapters")
+
+
+def hawq_logits(desc, x, past, past_lens, prompt_lens, starts, drafts, mask, penalties, bias_starts, bias_ids, bias_values, allowed, allowed_row, y, stream=None):
+    _check(load_library().hawq_logits(ctypes.byref(desc), _p(x), _p(past), _p(past_lens), _p(prompt_lens), _p(starts), _p(drafts), _p(mask), _p(penalties), _p(bias_starts),
+                                       _p(bias_ids), _p(bias_values), _p(allowed), _p(allowed_row), _p(y), _stream(stream)), "hawq_logits")
 
 
 def hawq_tune_set_tile(tile):

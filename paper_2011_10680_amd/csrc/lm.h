@@ -40,6 +40,9 @@ struct LinearW4Args {
     int32_t M, N, K, group, groups;
     int64_t x_stride, y_stride;
     int32_t dtype;
+    int32_t activation;            // of a gated pair: the rows of w, scales, zeros and bias from `up` on are its second projection
+    int64_t up;
+    float *sums;                   // workspace of a gated pair
 };
 
 struct AttnPromptArgs {
@@ -88,7 +91,47 @@ struct CacheStoreArgs {
     int64_t k_token, k_head, v_token, v_head;
 };
 
+struct RotaryArgs {
+    const void *x[2];              // queries, keys
+    void *y[2];
+    const int32_t *positions;
+    const double *turns;
+    int32_t total, q_heads, heads, head_dim, rotary_dim, layout, dtype;      // heads: of both
+    float scale;
+    int64_t x_token[2], x_head[2], y_token[2], y_head[2];
+};
+
+struct AdaptersArgs {
+    const void *x, *a, *b, *base;
+    const int32_t *ranks, *adapter;
+    const float *scales;
+    void *y;
+    float *h;                      // workspace: the rows' inner sums
+    int32_t M, N, K, n_adapters, max_rank, dtype;
+    int64_t x_stride, base_stride, y_stride, a_adapter, a_row, b_adapter, b_row;
+};
+
+struct LogitsArgs {
+    const void *x;
+    const int32_t *past, *past_lens, *prompt_lens, *starts, *drafts;
+    const uint64_t *mask;
+    const float *penalties;
+    const int32_t *bias_starts, *bias_ids;
+    const float *bias_values;
+    const uint32_t *allowed;
+    const int32_t *allowed_row;
+    void *y;
+    int32_t n_seqs, total, vocab, dtype, past_stride, n_bias, n_allowed;
+    int64_t allowed_stride, x_stride, y_stride;
+};
+
 hawq_status launch_linear_w4(const LinearW4Args &a, hipStream_t s);
+size_t gated_w4_workspace(const LinearW4Args &a);
+hawq_status launch_gated_w4(const LinearW4Args &a, hipStream_t s);
+hawq_status launch_rotary(const RotaryArgs &a, hipStream_t s);
+size_t adapters_workspace(const AdaptersArgs &a);
+hawq_status launch_adapters(const AdaptersArgs &a, hipStream_t s);
+hawq_status launch_logits(const LogitsArgs &a, hipStream_t s);
 hawq_status launch_attn_prompt(const AttnPromptArgs &a, hipStream_t s);
 size_t attn_tree_workspace(const AttnTreeArgs &a);
 hawq_status launch_attn_tree(const AttnTreeArgs &a, hipStream_t s);

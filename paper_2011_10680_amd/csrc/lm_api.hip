@@ -80,6 +80,42 @@ hawq_status tree_args(const hawq_attn_tree_desc *d, AttnTreeArgs &a) {
     return HAWQ_OK;
 }
 
+// y may be x: with the same strides
+bool same_place_ok(const void *x, int64_t x_token, int64_t x_head, const void *y, int64_t y_token, int64_t y_head) {
+    return x != y || !x || (x_token == y_token && x_head == y_head);
+}
+
+// stride of rows of n elements: of what is written, of what is read
+bool row_apart(int64_t stride, int64_t n) { return stride >= n && stride <= kMostStride; }
+bool row_read(int64_t stride, int64_t n) { return stride == 0 || row_apart(stride, n); }
+
+hawq_status gated_args(const hawq_gated_w4_desc *d, LinearW4Args &a) {
+    if (!d) return HAWQ_ERR_NULL;
+    if (d->M < 0 || d->N <= 0 || d->N > (1 << 30) || d->K <= 0 || (d->K & 1) || d->group <= 0 || d->group % 32 != 0) return HAWQ_ERR_SHAPE;
+    if (!row_read(d->x_stride, d->K) || !row_apart(d->y_stride, d->N)) return HAWQ_ERR_SHAPE;
+    if (!float16(d->x_dtype) || (d->w_dtype != HAWQ_S4 && d->w_dtype != HAWQ_U4)) return HAWQ_ERR_DTYPE;
+    if (d->activation < HAWQ_SILU || d->activation > HAWQ_RELU) return HAWQ_ERR_RANGE;
+    if (d->K > (1 << 25)) return HAWQ_ERR_UNSUPPORTED;
+    a = LinearW4Args{};
+    a.M = d->M; a.N = d->N; a.K = d->K; a.group = d->group; a.groups = (int32_t)(((int64_t)d->K + d->group - 1) / d->group);
+    a.x_stride = d->x_stride; a.y_stride = d->y_stride; a.dtype = d->x_dtype; a.activation = d->activation; a.up = d->N;
+    return HAWQ_OK;
+}
+
+hawq_status adapters_args(const hawq_adapters_desc *d, AdaptersArgs &a) {
+    if (!d) return HAWQ_ERR_NULL;
+    if (d->M < 0 || d->N <= 0 || d->K <= 0 || d->n_adapters < 0 || d->max_rank <= 0) return HAWQ_ERR_SHAPE;
+    if (!row_read(d->x_stride, d->K) || !row_read(d->base_stride, d->N) || !row_apart(d->y_stride, d->N)) return HAWQ_ERR_SHAPE;
+    if (!row_read(d->a_row, d->K) || !row_read(d->b_row, d->max_rank) || !strides_ok(d->a_adapter, d->b_adapter)) return HAWQ_ERR_SHAPE;
+    if (!float16(d->dtype)) return HAWQ_ERR_DTYPE;
+    if (d->K > kMostKeys || d->max_rank > (1 << 16)) return HAWQ_ERR_UNSUPPORTED;      // (counted in 32 bits, whole steps at a time)
+    a = AdaptersArgs{};
+    a.M = d->M; a.N = d->N; a.K = d->K; a.n_adapters = d->n_adapters; a.max_rank = d->max_rank; a.dtype = d->dtype;
+    a.x_stride = d->x_stride; a.base_stride = d->base_stride; a.y_stride = d->y_stride;
+    a.a_adapter = d->a_adapter; a.a_row = d->a_row; a.b_adapter = d->b_adapter; a.b_row = d->b_row;
+    return HAWQ_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -163,6 +199,96 @@ hawq_status hawq_cache_store(const hawq_cache_store_desc *d, const void *k, cons
     CacheStoreArgs a{k, v, slots, cache_args(d->cache, k_cache, v_cache, k_scales, v_scales), d->total, d->cache.kv_heads, d->cache.head_dim, d->dtype,
                      d->k_token, d->k_head, d->v_token, d->v_head};
     return launch_cache_store(a, (hipStream_t)stream);
+}
+
+hawq_status hawq_rotary(const hawq_rotary_desc *d, const void *q, const void *k, const int32_t *positions, const double *turns,
+                        void *yq, void *yk, void *stream) {
+    if (!d) return HAWQ_ERR_NULL;
+    if (d->total < 0 || d->q_heads < 0 || d->kv_heads < 0 || d->head_dim <= 0 || d->head_dim > 256) return HAWQ_ERR_SHAPE;
+    if (d->rotary_dim < 2 || d->rotary_dim > d->head_dim || (d->rotary_dim & 1)) return HAWQ_ERR_SHAPE;
+    if (!float16(d->dtype)) return HAWQ_ERR_DTYPE;
+    if (!std::isfinite(d->scale) || (d->layout != HAWQ_ROTARY_HALVES && d->layout != HAWQ_ROTARY_PAIRS)) return HAWQ_ERR_RANGE;
+    if (d->q_heads > 0 && (!strides_ok(d->q_token, d->q_head) || !rows_apart(d->yq_token, d->yq_head, d->total, d->q_heads, d->head_dim) ||
+                           !same_place_ok(q, d->q_token, d->q_head, yq, d->yq_token, d->yq_head)))
+        return HAWQ_ERR_SHAPE;
+    if (d->kv_heads > 0 && (!strides_ok(d->k_token, d->k_head) || !rows_apart(d->yk_token, d->yk_head, d->total, d->kv_heads, d->head_dim) ||
+                            !same_place_ok(k, d->k_token, d->k_head, yk, d->yk_token, d->yk_head)))
+        return HAWQ_ERR_SHAPE;
+    if (d->total == 0 || (d->q_heads == 0 && d->kv_heads == 0)) return HAWQ_OK;
+    if (d->q_heads > 65535 || d->kv_heads > 65535) return HAWQ_ERR_UNSUPPORTED;
+    if ((d->q_heads > 0 && (!q || !yq)) || (d->kv_heads > 0 && (!k || !yk)) || !positions || !turns) return HAWQ_ERR_NULL;
+    if ((d->q_heads > 0 && !at_multiple(2, {q, yq})) || (d->kv_heads > 0 && !at_multiple(2, {k, yk})) || !at_multiple(4, {positions}) || !at_multiple(8, {turns}))
+        return HAWQ_ERR_UNSUPPORTED;
+    RotaryArgs a{{q, k}, {yq, yk}, positions, turns, d->total, d->q_heads, d->q_heads + d->kv_heads, d->head_dim, d->rotary_dim, d->layout, d->dtype, d->scale,
+                 {d->q_token, d->k_token}, {d->q_head, d->k_head}, {d->yq_token, d->yk_token}, {d->yq_head, d->yk_head}};
+    return launch_rotary(a, (hipStream_t)stream);
+}
+
+size_t hawq_gated_w4_workspace_bytes(const hawq_gated_w4_desc *desc) {
+    LinearW4Args a;
+    return gated_args(desc, a) == HAWQ_OK ? gated_w4_workspace(a) : 0;
+}
+
+hawq_status hawq_gated_w4(const hawq_gated_w4_desc *d, const void *x, const void *w, const void *scales, const uint8_t *zeros,
+                          const void *bias, void *y, void *workspace, size_t workspace_bytes, void *stream) {
+    LinearW4Args a;
+    const hawq_status st = gated_args(d, a);
+    if (st != HAWQ_OK) return st;
+    if (d->w_dtype == HAWQ_S4 && zeros) return HAWQ_ERR_DTYPE;
+    if (d->M == 0) return HAWQ_OK;      // (an empty tensor has no address)
+    if (!x || !w || !scales || !y || (d->w_dtype == HAWQ_U4 && !zeros)) return HAWQ_ERR_NULL;
+    if (!at_multiple(2, {x, scales, bias, y})) return HAWQ_ERR_UNSUPPORTED;
+    const size_t need = gated_w4_workspace(a);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return workspace ? HAWQ_ERR_WORKSPACE : HAWQ_ERR_NULL;
+    if (need > 0 && !at_multiple(16, {workspace})) return HAWQ_ERR_UNSUPPORTED;
+    a.x = x; a.w = (const uint8_t *)w; a.scales = scales; a.zeros = zeros; a.bias = bias; a.y = y; a.sums = (float *)workspace;
+    return launch_gated_w4(a, (hipStream_t)stream);
+}
+
+size_t hawq_adapters_workspace_bytes(const hawq_adapters_desc *desc) {
+    AdaptersArgs a;
+    return adapters_args(desc, a) == HAWQ_OK ? adapters_workspace(a) : 0;
+}
+
+hawq_status hawq_adapters(const hawq_adapters_desc *d, const void *x, const void *a, const void *b, const int32_t *ranks, const float *scales,
+                          const int32_t *adapter, const void *base, void *y, void *workspace, size_t workspace_bytes, void *stream) {
+    AdaptersArgs args;
+    const hawq_status st = adapters_args(d, args);
+    if (st != HAWQ_OK) return st;
+    if (!same_place_ok(base, d->base_stride, 0, y, d->y_stride, 0)) return HAWQ_ERR_SHAPE;
+    if (d->M == 0) return HAWQ_OK;
+    if (!x || !adapter || !base || !y || (d->n_adapters > 0 && (!a || !b || !ranks || !scales))) return HAWQ_ERR_NULL;
+    if (!at_multiple(2, {x, a, b, base, y}) || !at_multiple(4, {ranks, scales, adapter})) return HAWQ_ERR_UNSUPPORTED;
+    const size_t need = adapters_workspace(args);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return workspace ? HAWQ_ERR_WORKSPACE : HAWQ_ERR_NULL;
+    if (need > 0 && !at_multiple(16, {workspace})) return HAWQ_ERR_UNSUPPORTED;
+    args.x = x; args.a = a; args.b = b; args.ranks = ranks; args.scales = scales; args.adapter = adapter; args.base = base; args.y = y; args.h = (float *)workspace;
+    return launch_adapters(args, (hipStream_t)stream);
+}
+
+hawq_status hawq_logits(const hawq_logits_desc *d, const void *x, const int32_t *past, const int32_t *past_lens, const int32_t *prompt_lens,
+                        const int32_t *starts, const int32_t *drafts, const uint64_t *mask, const float *penalties, const int32_t *bias_starts,
+                        const int32_t *bias_ids, const float *bias_values, const uint32_t *allowed, const int32_t *allowed_row, void *y, void *stream) {
+    if (!d) return HAWQ_ERR_NULL;
+    if (d->n_seqs < 0 || d->total < 0 || d->vocab <= 0 || d->past_stride < 0 || d->n_bias < 0 || d->n_allowed < 0) return HAWQ_ERR_SHAPE;
+    if (!row_read(d->x_stride, d->vocab) || !row_apart(d->y_stride, d->vocab) || !same_place_ok(x, d->x_stride, 0, y, d->y_stride, 0)) return HAWQ_ERR_SHAPE;
+    if (d->n_allowed > 0 && !row_read(d->allowed_stride, ((int64_t)d->vocab + 31) / 32)) return HAWQ_ERR_SHAPE;
+    if (!float16(d->dtype)) return HAWQ_ERR_DTYPE;
+    if (!starts && d->total != d->n_seqs) return HAWQ_ERR_SHAPE;
+    if (d->n_allowed > 0 && !allowed_row && d->n_allowed < d->total) return HAWQ_ERR_SHAPE;
+    if (d->n_seqs == 0 || d->total == 0) return HAWQ_OK;
+    if (!x || !y || (penalties && d->past_stride > 0 && (!past || !past_lens)) || (d->n_bias > 0 && (!bias_starts || !bias_ids || !bias_values)) ||
+        (d->n_allowed > 0 && !allowed))
+        return HAWQ_ERR_NULL;
+    if (!at_multiple(2, {x, y}) || !at_multiple(4, {starts, penalties}) || (penalties && !at_multiple(4, {past, past_lens, prompt_lens, drafts})) ||
+        (penalties && drafts && !at_multiple(8, {mask})) || (d->n_bias > 0 && !at_multiple(4, {bias_starts, bias_ids, bias_values})) ||
+        (d->n_allowed > 0 && !at_multiple(4, {allowed, allowed_row})))
+        return HAWQ_ERR_UNSUPPORTED;
+    LogitsArgs a{x, past, past_lens, prompt_lens, starts, drafts, mask, penalties, bias_starts, bias_ids, bias_values, allowed, allowed_row, y,
+                 d->n_seqs, d->total, d->vocab, d->dtype, d->past_stride, d->n_bias, d->n_allowed, d->allowed_stride, d->x_stride, d->y_stride};
+    if (!penalties || d->past_stride == 0) a.past = a.past_lens = a.prompt_lens = nullptr, a.past_stride = 0;
+    if (!penalties) a.drafts = nullptr;
+    return launch_logits(a, (hipStream_t)stream);
 }
 
 }  // extern "C"
