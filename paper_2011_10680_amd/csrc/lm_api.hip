@@ -16,6 +16,7 @@ bool at_multiple(int bytes, std::initializer_list<const void *> pointers) {
 }
 
 const int64_t kMostStride = (int64_t)1 << 40;
+const int kMostRows = INT32_MAX - 4095;     // and columns, where they are counted in 32 bits, whole tiles at a time
 const int kMostKeys = INT32_MAX - 255;      // of a row: the kernels count them in 32 bits, whole tiles at a time
 
 // strides of a tensor that is read: any that keep addresses inside 64 bits, 0 for a broadcast axis
@@ -108,7 +109,7 @@ hawq_status adapters_args(const hawq_adapters_desc *d, AdaptersArgs &a) {
     if (!row_read(d->x_stride, d->K) || !row_read(d->base_stride, d->N) || !row_apart(d->y_stride, d->N)) return HAWQ_ERR_SHAPE;
     if (!row_read(d->a_row, d->K) || !row_read(d->b_row, d->max_rank) || !strides_ok(d->a_adapter, d->b_adapter)) return HAWQ_ERR_SHAPE;
     if (!float16(d->dtype)) return HAWQ_ERR_DTYPE;
-    if (d->K > kMostKeys || d->max_rank > (1 << 16)) return HAWQ_ERR_UNSUPPORTED;      // (counted in 32 bits, whole steps at a time)
+    if (d->M > kMostRows || d->N > kMostRows || d->K > kMostRows || d->max_rank > (1 << 16)) return HAWQ_ERR_UNSUPPORTED;
     a = AdaptersArgs{};
     a.M = d->M; a.N = d->N; a.K = d->K; a.n_adapters = d->n_adapters; a.max_rank = d->max_rank; a.dtype = d->dtype;
     a.x_stride = d->x_stride; a.base_stride = d->base_stride; a.y_stride = d->y_stride;

@@ -87,6 +87,15 @@ def test_many_adapters_in_any_order_and_none():
     _run(1000, 32, 64, 2, 16, "bf16", adapter=[(i // 3) % 3 - 1 for i in range(1000)])
 
 
+@pytest.mark.parametrize("M,N,K,most", [(512, 300, 64, 64), (577, 33, 200, 8), (640, 1000, 72, 136), (1030, 64, 1000, 20)])
+def test_whole_prompts(M, N, K, most):
+    """Requests' rows one behind the other, and in between one in no order."""
+    for i, dtype in enumerate(("f16", "bf16")):
+        runs = [(j * 7 // M) % 4 - 1 for j in range(M)]
+        runs[200:260] = [(j * 5) % 4 - 1 for j in range(60)]
+        _run(M, N, K, 3, most, dtype, adapter=runs, in_place=i == 1, x_pad=8 * i, seed=M)
+
+
 def test_no_adapters_at_all():
     import torch
     import paper_2011_10680_amd as hawq
