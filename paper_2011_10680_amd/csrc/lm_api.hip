@@ -96,7 +96,7 @@ hawq_status gated_args(const hawq_gated_w4_desc *d, LinearW4Args &a) {
     if (!row_read(d->x_stride, d->K) || !row_apart(d->y_stride, d->N)) return HAWQ_ERR_SHAPE;
     if (!float16(d->x_dtype) || (d->w_dtype != HAWQ_S4 && d->w_dtype != HAWQ_U4)) return HAWQ_ERR_DTYPE;
     if (d->activation < HAWQ_SILU || d->activation > HAWQ_RELU) return HAWQ_ERR_RANGE;
-    if (d->K > (1 << 25)) return HAWQ_ERR_UNSUPPORTED;
+    if (d->M > kMostRows || d->K > (1 << 25)) return HAWQ_ERR_UNSUPPORTED;
     a = LinearW4Args{};
     a.M = d->M; a.N = d->N; a.K = d->K; a.group = d->group; a.groups = (int32_t)(((int64_t)d->K + d->group - 1) / d->group);
     a.x_stride = d->x_stride; a.y_stride = d->y_stride; a.dtype = d->x_dtype; a.activation = d->activation; a.up = d->N;
