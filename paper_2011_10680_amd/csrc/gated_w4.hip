@@ -70,60 +70,61 @@ __device__ __forceinline__ typename T::v8 expand_in_order(uint32_t d, uint32_t m
     return __builtin_bit_cast(typename T::v8, r);
 }
 
+constexpr int kStage = (kRows * 2 + 2 * kOuts / 2) * kStep, kGroups = 64;      // bytes of x and w of a step; groups whose scales are in LDS at once
+
 // PIECES: groups of 32 inputs (2) or of multiples of 64 (1)
 template <class T, int PIECES, bool ZEROS>
 __global__ __launch_bounds__(256, 2) void gated_prompt(LinearW4Args a, FastDiv by_group, int m_tiles, int tiles, int first_n) {
     typedef typename T::elem E;
-    __shared__ __align__(1024) char x_even[kRows * kStep * 2], x_odd[kRows * kStep * 2];
+    __shared__ __align__(1024) char stage0[kStage], stage1[kStage], stage2[kStage];
+    __shared__ __align__(16) E scale[kGroups][2 * kOuts];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int id = (int)xcd_remap(blockIdx.x, tiles), m0 = id % m_tiles * kRows, n0 = first_n + id / m_tiles * kOuts;
     const int wm = (wave >> 1) * 64, wn = (wave & 1) * 32, n = min(n0 + wn + col, a.N - 1);
     uint32_t mask = Nibbles<T>::mask, base = Nibbles<T>::base ^ (ZEROS ? 0u : Nibbles<T>::sign);
     asm("" : "+s"(mask));
     asm("" : "+v"(base));
+    // row of w, scales, zeros of column c of the workgroup, the second projection's behind the gate's
+    auto row_of = [&](int c) { return min(n0 + (c & (kOuts - 1)), a.N - 1) + (c >= kOuts ? a.up : 0); };
 
-    // direct loads: lane -> a row and a piece of 16 bytes of the wave's kilobyte; piece p of row r lies at p ^ (r & 7)
+    // direct loads of x: lane -> a row and a piece of 16 bytes of the wave's kilobyte; piece p of row r lies at p ^ (r & 7).  Of w: 16 bytes of
+    // a column's 32.
     const int lrow = wave * 8 + (lane >> 3), lpiece = (lane & 7) ^ (lrow & 7);
     const uint32_t x_off = (uint32_t)lrow * (uint32_t)a.x_stride * 2 + lpiece * 16;
     const int rows = min(kRows, a.M - m0);
     const E *x = (const E *)a.x + (int64_t)m0 * a.x_stride;
+    const int first_c = wave * 32 & (kOuts - 1), last_c = min(kOuts, a.N - n0) - 1, w_row = a.K >> 1;      // (a wave's 32 columns are of one projection)
+    const uint8_t *w = a.w + (n0 + (wave >= 2 ? a.up : 0)) * w_row;
+    const uint32_t w_off = (uint32_t)min(first_c + (lane >> 1), last_c) * (uint32_t)w_row + 16 * (lane & 1);
+    constexpr int kLoads = 5;                    // of a wave for a step
     auto fetch = [&](int k0, char *to) {
         const __amdgpu_buffer_rsrc_t rx = scalar_rsrc(x + k0, (uint32_t)(((rows - 1) * a.x_stride + a.K - k0) * 2));      // (rows past the last: zeros)
         const uint32_t off = k0 + 8 * lpiece < a.K ? x_off : 0x80000000u;
         for (int i = 0; i < 4; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void *)(to + i * 4096 + wave * 1024), 16, (int)(off + (uint32_t)(i * 32) * (uint32_t)a.x_stride * 2), 0, 0, 0);
+        const __amdgpu_buffer_rsrc_t rw = scalar_rsrc(w + (k0 >> 1), (uint32_t)(last_c * w_row + w_row - (k0 >> 1)));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (__attribute__((address_space(3))) void *)(to + kRows * kStep * 2 + wave * 1024), 16, (int)w_off, 0, 0, 0);
     };
-    fetch(0, x_even);
-
-    const uint8_t *w[2] = {a.w + (int64_t)n * (a.K >> 1), a.w + (n + a.up) * (a.K >> 1)};
-    const E *scales[2] = {(const E *)a.scales + (int64_t)n * a.groups, (const E *)a.scales + (n + a.up) * a.groups};
-    struct Stage {
-        v4u w[2];
-        float s[2][PIECES];
-    };
-    auto load = [&](int k0, Stage &g) {
-        for (int t = 0; t < 2; ++t) {
-            g.w[t] = *(const v4u *)(w[t] + (min(k0 + 32 * half, a.K - 32) >> 1));
-            for (int p = 0; p < PIECES; ++p) g.s[t][p] = (float)scales[t][fdiv((uint32_t)min(k0 + 32 * p, a.K - 1), by_group)];
-        }
-    };
-    Stage even, odd;
-    load(0, even);
 
     v16f acc[2][2];                              // [rows][projection]
     for (int i = 0; i < 2; ++i)
         for (int t = 0; t < 2; ++t)
             for (int e = 0; e < 16; ++e) acc[i][t][e] = 0;
     {
-        const uint8_t *zeros[2] = {ZEROS ? a.zeros + (int64_t)n * a.groups : nullptr, ZEROS ? a.zeros + (n + a.up) * a.groups : nullptr};
         const v4u *sums[2];
         for (int i = 0; i < 2; ++i) sums[i] = (const v4u *)a.sums + (int64_t)min(m0 + wm + 32 * i + col, a.M - 1) * a.groups;
+        const E *s[2];
+        const uint8_t *z[2] = {nullptr, nullptr};
+        for (int t = 0; t < 2; ++t) {
+            s[t] = (const E *)a.scales + (n + t * a.up) * a.groups;
+            if (ZEROS) z[t] = a.zeros + (n + t * a.up) * a.groups;
+        }
         for (int q = 0; q < a.groups; q += 2) {
             const int g = min(q + half, a.groups - 1);
             const uint32_t there = q + half < a.groups ? ~0u : 0u;
             v4u xs[2], ws[2];
             for (int i = 0; i < 2; ++i) xs[i] = sums[i][g] & there;
-            for (int t = 0; t < 2; ++t) ws[t] = two_parts(-(float)scales[t][g] * (float)(16 + (ZEROS ? zeros[t][g] : 8))) & there;
+            for (int t = 0; t < 2; ++t) ws[t] = two_parts(-(float)s[t][g] * (float)(16 + (ZEROS ? z[t][g] : 8))) & there;
             for (int i = 0; i < 2; ++i)
                 for (int t = 0; t < 2; ++t) acc[i][t] = BF16::mfma32(__builtin_bit_cast(BF16::v8, xs[i]), __builtin_bit_cast(BF16::v8, ws[t]), acc[i][t]);
         }
@@ -131,12 +132,19 @@ __global__ __launch_bounds__(256, 2) void gated_prompt(LinearW4Args a, FastDiv b
 
     int x_at[4];                                 // operand reads: pieces 2 half + (0, 1) of the row's first and second 32 inputs
     for (int p = 0; p < 4; ++p) x_at[p] = (wm + col) * 128 + (((4 * (p >> 1) + 2 * half + (p & 1)) ^ (col & 7)) << 4);
-    auto use = [&](Stage &g, const char *xs) {
+    const int w_at = kRows * kStep * 2 + (wn + col) * 32 + half * 16;
+    auto use = [&](int k0, int g0, const char *at) {
         typename T::v8 wv[2][4], xv[2][4];
         for (int i = 0; i < 2; ++i)
-            for (int p = 0; p < 4; ++p) xv[i][p] = *(const typename T::v8 *)(xs + x_at[p] + i * 32 * 128);
+            for (int p = 0; p < 4; ++p) xv[i][p] = *(const typename T::v8 *)(at + x_at[p] + i * 32 * 128);
+        float sc[2][PIECES];
+        for (int p = 0; p < PIECES; ++p) {
+            const int g = (int)fdiv((uint32_t)min(k0 + 32 * p, a.K - 1), by_group) - g0;
+            for (int t = 0; t < 2; ++t) sc[t][p] = (float)scale[g][t * kOuts + wn + col];
+        }
         for (int t = 0; t < 2; ++t) {
-            const v2u u = __builtin_amdgcn_permlane32_swap(g.w[t].x, g.w[t].z, false, false), v = __builtin_amdgcn_permlane32_swap(g.w[t].y, g.w[t].w, false, false);
+            const v4u d = *(const v4u *)(at + w_at + t * kOuts * 32);
+            const v2u u = __builtin_amdgcn_permlane32_swap(d.x, d.z, false, false), v = __builtin_amdgcn_permlane32_swap(d.y, d.w, false, false);
             wv[t][0] = expand_in_order<T>(u.x, mask, base);
             wv[t][1] = expand_in_order<T>(v.x, mask, base);
             wv[t][2] = expand_in_order<T>(u.y, mask, base);
@@ -148,19 +156,36 @@ __global__ __launch_bounds__(256, 2) void gated_prompt(LinearW4Args a, FastDiv b
                     v16f part;
                     for (int e = 0; e < 16; ++e) part[e] = 0;
                     for (int j = p * 4 / PIECES; j < (p + 1) * 4 / PIECES; ++j) part = T::mfma32(xv[i][j], wv[t][j], part);
-                    for (int e = 0; e < 16; ++e) acc[i][t][e] = fmaf(g.s[t][p], part[e], acc[i][t][e]);
+                    for (int e = 0; e < 16; ++e) acc[i][t][e] = fmaf(sc[t][p], part[e], acc[i][t][e]);
                 }
     };
-    for (int k = 0; k < a.K; k += 2 * kStep) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    for (int g0 = 0; g0 < a.groups; g0 += kGroups) {
+        const int n_groups = min(kGroups, a.groups - g0), first = g0 * a.group, last = (int)min((int64_t)first + (int64_t)n_groups * a.group, (int64_t)a.K);
         __syncthreads();
-        if (k + kStep < a.K) fetch(k + kStep, x_odd), load(k + kStep, odd);
-        use(even, x_even);
-        if (k + kStep >= a.K) break;
+        for (int i = threadIdx.x; i < n_groups * 2 * kOuts; i += 256) {
+            const int c = i & (2 * kOuts - 1), g = i / (2 * kOuts);
+            scale[g][c] = ((const E *)a.scales)[row_of(c) * a.groups + g0 + g];
+        }
+        fetch(first, stage0);
+        fetch(min(first + kStep, a.K - 32), stage1);
+        // Three steps in turn: what the step needs has landed when no more than the next one's loads are under way; the one two ahead then
+        // takes the place of the step before, which all waves have left behind.  (Past the end the last inputs are fetched again: with loads in
+        // a branch the compiler would wait for all of them.)
+        auto turn = [&](int k, const char *now, char *then) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads) : "memory");
+            __builtin_amdgcn_s_barrier();        // (__syncthreads would wait for the next step's loads too)
+            asm volatile("" ::: "memory");
+            fetch(min(k + 2 * kStep, a.K - 32), then);
+            use(k, g0, now);
+        };
+        for (int k = first; k < last; k += 3 * kStep) {
+            turn(k, stage0, stage2);
+            if (k + kStep >= last) break;
+            turn(k + kStep, stage1, stage0);
+            if (k + 2 * kStep >= last) break;
+            turn(k + 2 * kStep, stage2, stage1);
+        }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (k + 2 * kStep < a.K) fetch(k + 2 * kStep, x_even), load(k + 2 * kStep, even);
-        use(odd, x_odd);
     }
 
     const bool inside = n0 + wn + col < a.N;
