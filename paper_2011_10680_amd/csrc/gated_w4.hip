@@ -1,7 +1,7 @@
 // The first half of a gated feed-forward block from 4-bit weights, act(x Wg^T) * (x Wu^T): for few rows the linear layer's kernel with both
 // projections in a workgroup (linear_w4.h), for whole prompts the kernel below.
 //
-// Prompt kernel.  A workgroup of four waves takes 128 rows and 64 outputs, a wave 64 rows and the 32 + 32 columns of its outputs' two
+// Prompt kernel.  A workgroup of eight waves takes 128 rows and 128 outputs, a wave 64 rows and the 32 + 32 columns of its outputs' two
 // projections, so that gate and second projection of an output meet in one lane and only their product is stored.  As in linear_w4.h a
 // weight is 16 + nibble in the mantissa of a 16-bit float, and a group's part is scaled in 32 bits:
 //   g[m,n] = sum_g s[n,g] * ( sum_k x[m,k] u[n,k] )  -  sum_g ( s[n,g] (16 + z[n,g]) ) * ( sum_{k in g} x[m,k] )
@@ -18,7 +18,7 @@ namespace hawq {
 
 namespace {
 
-constexpr int kRows = 128, kOuts = 64, kStep = 64;
+constexpr int kRows = 128, kOuts = 128, kStep = 64, kThreads = 512;
 constexpr int kMostInputs = 1 << 16, kMostXStride = 1 << 22;       // of the prompt kernel: 32-bit offsets, a row's sums in LDS
 
 // v as three bf16 parts, each the one below its rest's (towards zero), and the operand {1, 1, 2, 2, 3, 0, 0, 0} of them
@@ -70,80 +70,85 @@ __device__ __forceinline__ typename T::v8 expand_in_order(uint32_t d, uint32_t m
     return __builtin_bit_cast(typename T::v8, r);
 }
 
-constexpr int kStage = (kRows * 2 + 2 * kOuts / 2) * kStep, kGroups = 64;      // bytes of x and w of a step; groups whose scales are in LDS at once
+constexpr int kBlock = 2 * kStep, kGroups = 64;  // inputs whose weights are fetched together; groups whose scales are in LDS at once
+constexpr int kSide = 4;                         // row tiles side by side in the order of the tiles
 
-// PIECES: groups of 32 inputs (2) or of multiples of 64 (1)
-template <class T, int PIECES, bool ZEROS>
-__global__ __launch_bounds__(256, 2) void gated_prompt(LinearW4Args a, FastDiv by_group, int m_tiles, int tiles, int first_n) {
+// Scales and zero points of a workgroup's columns: rows of 33 and 17 words, so that a column's scale and its neighbours' lie in different
+// banks.  unread: a direct load goes there once, since the compiler has a read of LDS that no direct load has written to wait for all that
+// are under way, and the scales' would wait for the next steps' x.
+template <class E, bool ZEROS>
+struct Side {
+    E scale[2 * kOuts][kGroups + 2];
+    uint8_t zero[ZEROS ? 2 * kOuts : 1][kGroups + 4];
+    uint32_t unread[64];
+};
+
+// PARTS: how often a group's part of 128 inputs is scaled: 1, 2 or 4 times, for groups of multiples of 128, 64 and 32
+template <class T, int PARTS, bool ZEROS>
+__global__ __launch_bounds__(kThreads, 2) void gated_prompt(LinearW4Args a, FastDiv by_group, int m_tiles, int tiles, int first_n) {
     typedef typename T::elem E;
-    __shared__ __align__(1024) char stage0[kStage], stage1[kStage], stage2[kStage];
-    __shared__ __align__(16) E scale[kGroups][2 * kOuts];
+    __shared__ __align__(1024) char x0[kRows * kStep * 2], x1[kRows * kStep * 2], x2[kRows * kStep * 2], x3[kRows * kStep * 2], w0[kOuts * kBlock], w1[kOuts * kBlock];
+    __shared__ __align__(16) Side<E, ZEROS> lds;
+    auto &scale = lds.scale;
+    auto &zero = lds.zero;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
-    const int id = (int)xcd_remap(blockIdx.x, tiles), m0 = id % m_tiles * kRows, n0 = first_n + id / m_tiles * kOuts;
-    const int wm = (wave >> 1) * 64, wn = (wave & 1) * 32, n = min(n0 + wn + col, a.N - 1);
+    // An XCD's workgroups at one time are some tiles of rows by some of outputs: 4 by 8 read 4 MB of x and 4 of w, 16 by 2 would read 17.
+    const int id = (int)xcd_remap(blockIdx.x, tiles), set = id / (kSide * (tiles / m_tiles)), in_set = id - set * kSide * (tiles / m_tiles), side = min(kSide, m_tiles - set * kSide);
+    const int m0 = (set * kSide + in_set % side) * kRows, n0 = first_n + in_set / side * kOuts;
+    const int wm = (wave >> 2) * 64, wn = (wave & 3) * 32, n = min(n0 + wn + col, a.N - 1);
     uint32_t mask = Nibbles<T>::mask, base = Nibbles<T>::base ^ (ZEROS ? 0u : Nibbles<T>::sign);
     asm("" : "+s"(mask));
     asm("" : "+v"(base));
     // row of w, scales, zeros of column c of the workgroup, the second projection's behind the gate's
     auto row_of = [&](int c) { return min(n0 + (c & (kOuts - 1)), a.N - 1) + (c >= kOuts ? a.up : 0); };
 
-    // direct loads of x: lane -> a row and a piece of 16 bytes of the wave's kilobyte; piece p of row r lies at p ^ (r & 7).  Of w: 16 bytes of
-    // a column's 32.
-    const int lrow = wave * 8 + (lane >> 3), lpiece = (lane & 7) ^ (lrow & 7);
-    const uint32_t x_off = (uint32_t)lrow * (uint32_t)a.x_stride * 2 + lpiece * 16;
+    // Direct loads, a kilobyte of a wave at a time.  x: lane -> a row and a piece of 16 bytes; piece p of row r lies at p ^ (r / 2 & 7), so that
+    // 16 rows' reads meet every bank once.  Weights of a block: lane -> a column and a piece of its 64 bytes, piece p of column c at p ^ (c / 4 & 3).
+    const int x_row = wave * 8 + (lane >> 3), x_piece = (lane & 7) ^ (x_row >> 1 & 7);
+    const uint32_t x_off = (uint32_t)x_row * (uint32_t)a.x_stride * 2 + x_piece * 16;
     const int rows = min(kRows, a.M - m0);
     const E *x = (const E *)a.x + (int64_t)m0 * a.x_stride;
-    const int first_c = wave * 32 & (kOuts - 1), last_c = min(kOuts, a.N - n0) - 1, w_row = a.K >> 1;      // (a wave's 32 columns are of one projection)
-    const uint8_t *w = a.w + (n0 + (wave >= 2 ? a.up : 0)) * w_row;
-    const uint32_t w_off = (uint32_t)min(first_c + (lane >> 1), last_c) * (uint32_t)w_row + 16 * (lane & 1);
-    constexpr int kLoads = 5;                    // of a wave for a step
-    auto fetch = [&](int k0, char *to) {
-        const __amdgpu_buffer_rsrc_t rx = scalar_rsrc(x + k0, (uint32_t)(((rows - 1) * a.x_stride + a.K - k0) * 2));      // (rows past the last: zeros)
-        const uint32_t off = k0 + 8 * lpiece < a.K ? x_off : 0x80000000u;
-        for (int i = 0; i < 4; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void *)(to + i * 4096 + wave * 1024), 16, (int)(off + (uint32_t)(i * 32) * (uint32_t)a.x_stride * 2), 0, 0, 0);
+    auto fetch_x = [&](int k, char *to) {        // (rows and inputs past the last: zeros)
+        const int k0 = min(k, a.K - 32);
+        const __amdgpu_buffer_rsrc_t rx = scalar_rsrc(x + k0, (uint32_t)(((rows - 1) * a.x_stride + a.K - k0) * 2));
+        const uint32_t off = k + 8 * x_piece < a.K ? x_off : 0x80000000u;
+        for (int i = 0; i < 2; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void *)(to + i * 8192 + wave * 1024), 16, (int)(off + (uint32_t)(i * 64) * (uint32_t)a.x_stride * 2), 0, 0, 0);
+    };
+    const int last_c = min(kOuts, a.N - n0) - 1, w_row = a.K >> 1, w_col = wave * 32 + (lane >> 2) & (kOuts - 1);      // (a wave's 32 columns are of one projection)
+    const uint8_t *w = a.w + (n0 + (wave >= 4 ? a.up : 0)) * w_row;
+    const int w_piece = (lane & 3) ^ (lane >> 4 & 3);
+    auto fetch_w = [&](int k, char *to) {        // (columns past the last: the last one's; inputs past the last: whatever there is)
+        const int k0 = min(k, a.K - 32);
         const __amdgpu_buffer_rsrc_t rw = scalar_rsrc(w + (k0 >> 1), (uint32_t)(last_c * w_row + w_row - (k0 >> 1)));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (__attribute__((address_space(3))) void *)(to + kRows * kStep * 2 + wave * 1024), 16, (int)w_off, 0, 0, 0);
+        for (int i = 0; i < 2; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (__attribute__((address_space(3))) void *)(to + wave * 2048 + i * 1024), 16,
+                                                     (int)((uint32_t)min(w_col + 16 * i, last_c) * (uint32_t)w_row + 16 * w_piece), 0, 0, 0);
     };
 
     v16f acc[2][2];                              // [rows][projection]
     for (int i = 0; i < 2; ++i)
         for (int t = 0; t < 2; ++t)
             for (int e = 0; e < 16; ++e) acc[i][t][e] = 0;
-    {
-        const v4u *sums[2];
-        for (int i = 0; i < 2; ++i) sums[i] = (const v4u *)a.sums + (int64_t)min(m0 + wm + 32 * i + col, a.M - 1) * a.groups;
-        const E *s[2];
-        const uint8_t *z[2] = {nullptr, nullptr};
-        for (int t = 0; t < 2; ++t) {
-            s[t] = (const E *)a.scales + (n + t * a.up) * a.groups;
-            if (ZEROS) z[t] = a.zeros + (n + t * a.up) * a.groups;
-        }
-        for (int q = 0; q < a.groups; q += 2) {
-            const int g = min(q + half, a.groups - 1);
-            const uint32_t there = q + half < a.groups ? ~0u : 0u;
-            v4u xs[2], ws[2];
-            for (int i = 0; i < 2; ++i) xs[i] = sums[i][g] & there;
-            for (int t = 0; t < 2; ++t) ws[t] = two_parts(-(float)s[t][g] * (float)(16 + (ZEROS ? z[t][g] : 8))) & there;
-            for (int i = 0; i < 2; ++i)
-                for (int t = 0; t < 2; ++t) acc[i][t] = BF16::mfma32(__builtin_bit_cast(BF16::v8, xs[i]), __builtin_bit_cast(BF16::v8, ws[t]), acc[i][t]);
-        }
-    }
-
     int x_at[4];                                 // operand reads: pieces 2 half + (0, 1) of the row's first and second 32 inputs
-    for (int p = 0; p < 4; ++p) x_at[p] = (wm + col) * 128 + (((4 * (p >> 1) + 2 * half + (p & 1)) ^ (col & 7)) << 4);
-    const int w_at = kRows * kStep * 2 + (wn + col) * 32 + half * 16;
-    auto use = [&](int k0, int g0, const char *at) {
+    for (int p = 0; p < 4; ++p) x_at[p] = (wm + col) * 128 + (((4 * (p >> 1) + 2 * half + (p & 1)) ^ (col >> 1 & 7)) << 4);
+    int w_at[2];                                 // pieces half and 2 + half of the column's 64 bytes
+    for (int s = 0; s < 2; ++s) w_at[s] = (wn + col) * 64 + (((2 * s + half) ^ (col >> 2 & 3)) << 4);
+    // the 64 inputs from k on, the first or second of a block's two steps
+    v16f part[2][2];
+    auto use = [&](auto second, int k, int g0, const char *xs, const char *ws) {
+        constexpr bool kSecond = decltype(second)::value;
+        constexpr int PIECES = PARTS == 4 ? 2 : 1;
         typename T::v8 wv[2][4], xv[2][4];
         for (int i = 0; i < 2; ++i)
-            for (int p = 0; p < 4; ++p) xv[i][p] = *(const typename T::v8 *)(at + x_at[p] + i * 32 * 128);
+            for (int p = 0; p < 4; ++p) xv[i][p] = *(const typename T::v8 *)(xs + x_at[p] + i * 32 * 128);
         float sc[2][PIECES];
         for (int p = 0; p < PIECES; ++p) {
-            const int g = (int)fdiv((uint32_t)min(k0 + 32 * p, a.K - 1), by_group) - g0;
-            for (int t = 0; t < 2; ++t) sc[t][p] = (float)scale[g][t * kOuts + wn + col];
+            const int g = (int)fdiv((uint32_t)min(k + 32 * p, a.K - 1), by_group) - g0;
+            for (int t = 0; t < 2; ++t) sc[t][p] = (float)scale[t * kOuts + wn + col][g];
         }
         for (int t = 0; t < 2; ++t) {
-            const v4u d = *(const v4u *)(at + w_at + t * kOuts * 32);
+            const v4u d = *(const v4u *)(ws + w_at[kSecond] + t * kOuts * 64);
             const v2u u = __builtin_amdgcn_permlane32_swap(d.x, d.z, false, false), v = __builtin_amdgcn_permlane32_swap(d.y, d.w, false, false);
             wv[t][0] = expand_in_order<T>(u.x, mask, base);
             wv[t][1] = expand_in_order<T>(v.x, mask, base);
@@ -151,39 +156,84 @@ __global__ __launch_bounds__(256, 2) void gated_prompt(LinearW4Args a, FastDiv b
             wv[t][3] = expand_in_order<T>(v.y, mask, base);
         }
         for (int t = 0; t < 2; ++t)
-            for (int i = 0; i < 2; ++i)
-                for (int p = 0; p < PIECES; ++p) {
-                    v16f part;
-                    for (int e = 0; e < 16; ++e) part[e] = 0;
-                    for (int j = p * 4 / PIECES; j < (p + 1) * 4 / PIECES; ++j) part = T::mfma32(xv[i][j], wv[t][j], part);
-                    for (int e = 0; e < 16; ++e) acc[i][t][e] = fmaf(sc[t][p], part[e], acc[i][t][e]);
+            for (int p = 0; p < PIECES; ++p)
+                for (int i = 0; i < 2; ++i) {
+                    v16f &sum = part[i][t];
+                    if (PARTS > 1 || !kSecond)
+                        for (int e = 0; e < 16; ++e) sum[e] = 0;
+                    for (int j = p * 4 / PIECES; j < (p + 1) * 4 / PIECES; ++j) sum = T::mfma32(xv[i][j], wv[t][j], sum);
+                    if (PARTS > 1 || kSecond)
+                        for (int e = 0; e < 16; ++e) acc[i][t][e] = fmaf(sc[t][p], sum[e], acc[i][t][e]);
                 }
     };
     for (int g0 = 0; g0 < a.groups; g0 += kGroups) {
         const int n_groups = min(kGroups, a.groups - g0), first = g0 * a.group, last = (int)min((int64_t)first + (int64_t)n_groups * a.group, (int64_t)a.K);
+        const int blocks = (last - first + kBlock - 1) / kBlock;
         __syncthreads();
-        for (int i = threadIdx.x; i < n_groups * 2 * kOuts; i += 256) {
-            const int c = i & (2 * kOuts - 1), g = i / (2 * kOuts);
-            scale[g][c] = ((const E *)a.scales)[row_of(c) * a.groups + g0 + g];
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(scalar_rsrc(w, 4), (__attribute__((address_space(3))) void *)lds.unread, 4, 0, 0, 0, 0);
+        fetch_w(first, w0);
+        // The second term: eight groups' sums of the rows in the place of a step of x, 32 groups at a time.
+        for (int q0 = 0; q0 < n_groups; q0 += 32) {
+            if (q0 > 0) __syncthreads();
+            // (by registers: a direct load here would have the compiler wait for all of them in the loop below)
+            v4u in[8];
+            for (int i = 0; i < 8; ++i) {
+                const int r = x_row + 64 * (i & 1), g = g0 + q0 + 8 * (i >> 1) + x_piece;
+                in[i] = ((const v4u *)a.sums)[(int64_t)min(m0 + r, a.M - 1) * a.groups + min(g, a.groups - 1)];
+                if (g >= a.groups) in[i] = v4u{0, 0, 0, 0};
+            }
+            for (int i = 0; i < 8; ++i) *(v4u *)((i < 2 ? x0 : i < 4 ? x1 : i < 6 ? x2 : x3) + (i & 1) * 8192 + threadIdx.x * 16) = in[i];
+            // and a thread brings sixteen scales and zero points of a column to LDS
+            const int c = threadIdx.x >> 1;
+            const int64_t row = row_of(c) * a.groups + g0;
+            const int g1 = q0 + 16 * (threadIdx.x & 1);
+            for (int e = 0; e < 16; ++e) scale[c][g1 + e] = ((const E *)a.scales)[row + min(g1 + e, n_groups - 1)];
+            if (ZEROS)
+                for (int e = 0; e < 16; ++e) zero[c][g1 + e] = a.zeros[row + min(g1 + e, n_groups - 1)];
+            __syncthreads();
+            auto subtract = [&](int g1, const char *from) {
+                for (int q = 0; q < 4; ++q) {
+                    const int g = g1 + 2 * q + half;
+                    BF16::v8 xs[2], ws[2];
+                    for (int i = 0; i < 2; ++i) xs[i] = *(const BF16::v8 *)(from + (wm + 32 * i + col) * 128 + (((2 * q + half) ^ (col >> 1 & 7)) << 4));
+                    for (int t = 0; t < 2; ++t) {
+                        const int c = t * kOuts + wn + col;
+                        ws[t] = __builtin_bit_cast(BF16::v8, two_parts(-(float)scale[c][g] * (float)(16 + (ZEROS ? zero[c][g] : 8))));
+                    }
+                    for (int i = 0; i < 2; ++i)
+                        for (int t = 0; t < 2; ++t) acc[i][t] = BF16::mfma32(xs[i], ws[t], acc[i][t]);
+                }
+            };
+            subtract(q0, x0);
+            if (q0 + 8 < n_groups) subtract(q0 + 8, x1);
+            if (q0 + 16 < n_groups) subtract(q0 + 16, x2);
+            if (q0 + 24 < n_groups) subtract(q0 + 24, x3);
         }
-        fetch(first, stage0);
-        fetch(min(first + kStep, a.K - 32), stage1);
-        // Three steps in turn: what the step needs has landed when no more than the next one's loads are under way; the one two ahead then
-        // takes the place of the step before, which all waves have left behind.  (Past the end the last inputs are fetched again: with loads in
-        // a branch the compiler would wait for all of them.)
-        auto turn = [&](int k, const char *now, char *then) {
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads) : "memory");
-            __builtin_amdgcn_s_barrier();        // (__syncthreads would wait for the next step's loads too)
+        __syncthreads();
+        fetch_x(first, x0);
+        fetch_x(first + kStep, x1);
+        fetch_x(first + kBlock, x2);
+        asm volatile("s_waitcnt vmcnt(4)" ::: "memory");      // (w0: the loads counted below are the only ones under way)
+        // Steps of 64 inputs, x three steps ahead and the weights of a block two: what a step needs has landed when no more than the loads behind
+        // it are under way, and what is fetched takes the place of what all waves have left behind.  (Past the end zeros are fetched: with
+        // loads in a branch the compiler would wait for all of them.)
+        auto turn = [&](auto allowed, auto second, int k, const char *xs, const char *ws, char *x_to, char *w_to) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(allowed)::value) : "memory");
+            __builtin_amdgcn_s_barrier();        // (__syncthreads would wait for all loads)
             asm volatile("" ::: "memory");
-            fetch(min(k + 2 * kStep, a.K - 32), then);
-            use(k, g0, now);
+            if (!decltype(second)::value) fetch_w(k + kBlock, w_to);
+            fetch_x(k + 3 * kStep, x_to);
+            __builtin_amdgcn_sched_barrier(0);   // (else they are put off to the products' end)
+            use(second, k, g0, xs, ws);
         };
-        for (int k = first; k < last; k += 3 * kStep) {
-            turn(k, stage0, stage2);
-            if (k + kStep >= last) break;
-            turn(k + kStep, stage1, stage0);
-            if (k + 2 * kStep >= last) break;
-            turn(k + 2 * kStep, stage2, stage1);
+        typedef std::integral_constant<int, 4> Four;
+        typedef std::integral_constant<int, 6> Six;
+        for (int k = first; k < last; k += 2 * kBlock) {
+            turn(Four(), std::false_type(), k, x0, w0, x3, w1);
+            turn(Six(), std::true_type(), k + kStep, x1, w0, x0, nullptr);
+            if (k + kBlock >= last) break;
+            turn(Four(), std::false_type(), k + kBlock, x2, w1, x1, w0);
+            turn(Six(), std::true_type(), k + kBlock + kStep, x3, w1, x2, nullptr);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
@@ -227,17 +277,18 @@ hawq_status launch_prompt(const LinearW4Args &a, hipStream_t s) {
     group_sums<T><<<dim3((unsigned)rows.x, (unsigned)rows.y), 256, 0, s>>>(a);
     hawq_status st = check_launch();
     if (st != HAWQ_OK) return st;
-    const int64_t m_tiles = ((int64_t)a.M + kRows - 1) / kRows, n_tiles = ((int64_t)a.N + kOuts - 1) / kOuts, at_once = most_blocks(256) / m_tiles;
+    const int64_t m_tiles = ((int64_t)a.M + kRows - 1) / kRows, n_tiles = ((int64_t)a.N + kOuts - 1) / kOuts, at_once = most_blocks(kThreads) / m_tiles;
     const FastDiv by_group = fast_div((uint32_t)a.group);
     for (int64_t n = 0; n < n_tiles; n += at_once) {                     // as many outputs as a launch holds
         const int tiles = (int)(m_tiles * (n_tiles - n < at_once ? n_tiles - n : at_once)), first_n = (int)n * kOuts;
-        if (a.group % 64 == 0) {
-            if (a.zeros) gated_prompt<T, 1, true><<<dim3((unsigned)tiles), 256, 0, s>>>(a, by_group, (int)m_tiles, tiles, first_n);
-            else gated_prompt<T, 1, false><<<dim3((unsigned)tiles), 256, 0, s>>>(a, by_group, (int)m_tiles, tiles, first_n);
-        } else {
-            if (a.zeros) gated_prompt<T, 2, true><<<dim3((unsigned)tiles), 256, 0, s>>>(a, by_group, (int)m_tiles, tiles, first_n);
-            else gated_prompt<T, 2, false><<<dim3((unsigned)tiles), 256, 0, s>>>(a, by_group, (int)m_tiles, tiles, first_n);
-        }
+        const auto go = [&](auto parts) {
+            constexpr int PARTS = decltype(parts)::value;
+            if (a.zeros) gated_prompt<T, PARTS, true><<<dim3((unsigned)tiles), kThreads, 0, s>>>(a, by_group, (int)m_tiles, tiles, first_n);
+            else gated_prompt<T, PARTS, false><<<dim3((unsigned)tiles), kThreads, 0, s>>>(a, by_group, (int)m_tiles, tiles, first_n);
+        };
+        if (a.group % 128 == 0) go(std::integral_constant<int, 1>());
+        else if (a.group % 64 == 0) go(std::integral_constant<int, 2>());
+        else go(std::integral_constant<int, 4>());
         st = check_launch();
         if (st != HAWQ_OK) return st;
     }

@@ -85,11 +85,18 @@ __device__ __forceinline__ double plain_output(const LinearW4Args &a, int m, int
     return v;
 }
 
+// exp(v): v log2(e) as a product and what rounding it left out (2 units in the last place; one of 30 alone would be off by 20)
+__device__ __forceinline__ float exp_of(float v) {
+    const float t = v * 1.44269504f, rest = fmaf(v, 1.92596303e-8f, fmaf(v, 1.44269504f, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fabsf(t) < 126.f ? fmaf(e, rest * 0.693147181f, e) : e;
+}
+
 // The gate's activation.  The normal distribution's tail is taken by itself, not as a difference from 1.
 __device__ __forceinline__ float activated(float g, int kind) {
-    if (kind == HAWQ_SILU) return g / (1.f + expf(-g));
+    if (kind == HAWQ_SILU) return g * __builtin_amdgcn_rcpf(1.f + exp_of(-g));
     if (kind == HAWQ_GELU) return 0.5f * g * erfcf(g * -0.70710678118654752f);
-    if (kind == HAWQ_GELU_TANH) return g / (1.f + expf(-1.5957691216057308f * (g + 0.044715f * g * g * g)));      // (1 + tanh t) / 2 = 1 / (1 + exp(-2 t))
+    if (kind == HAWQ_GELU_TANH) return g * __builtin_amdgcn_rcpf(1.f + exp_of(-1.5957691216057308f * (g + 0.044715f * g * g * g)));      // (1 + tanh t) / 2 = 1 / (1 + exp(-2 t))
     return g > 0.f || g != g ? g : 0.f;
 }
 
