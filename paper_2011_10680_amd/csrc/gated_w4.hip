@@ -134,27 +134,30 @@ __global__ __launch_bounds__(kThreads, 2) void gated_prompt(LinearW4Args a, Fast
     for (int p = 0; p < 4; ++p) x_at[p] = (wm + col) * 128 + (((4 * (p >> 1) + 2 * half + (p & 1)) ^ (col >> 1 & 7)) << 4);
     int w_at[2];                                 // pieces half and 2 + half of the column's 64 bytes
     for (int s = 0; s < 2; ++s) w_at[s] = (wn + col) * 64 + (((2 * s + half) ^ (col >> 2 & 3)) << 4);
-    // the 64 inputs from k on, the first or second of a block's two steps
+    // Operands of the 64 inputs from k on, the first or second of a block's two steps, and their products.
+    constexpr int PIECES = PARTS == 4 ? 2 : 1;
+    typename T::v8 wv[2][4], xv[2][4];
+    float sc[2][PIECES];
     v16f part[2][2];
-    auto use = [&](auto second, int k, int g0, const char *xs, const char *ws) {
-        constexpr bool kSecond = decltype(second)::value;
-        constexpr int PIECES = PARTS == 4 ? 2 : 1;
-        typename T::v8 wv[2][4], xv[2][4];
-        for (int i = 0; i < 2; ++i)
-            for (int p = 0; p < 4; ++p) xv[i][p] = *(const typename T::v8 *)(xs + x_at[p] + i * 32 * 128);
-        float sc[2][PIECES];
+    auto read = [&](auto second, int k, int g0, const char *xs, const char *ws) {
+        v4u d[2];
+        for (int t = 0; t < 2; ++t) d[t] = *(const v4u *)(ws + w_at[decltype(second)::value] + t * kOuts * 64);
         for (int p = 0; p < PIECES; ++p) {
             const int g = (int)fdiv((uint32_t)min(k + 32 * p, a.K - 1), by_group) - g0;
             for (int t = 0; t < 2; ++t) sc[t][p] = (float)scale[t * kOuts + wn + col][g];
         }
+        for (int i = 0; i < 2; ++i)
+            for (int p = 0; p < 4; ++p) xv[i][p] = *(const typename T::v8 *)(xs + x_at[p] + i * 32 * 128);
         for (int t = 0; t < 2; ++t) {
-            const v4u d = *(const v4u *)(ws + w_at[kSecond] + t * kOuts * 64);
-            const v2u u = __builtin_amdgcn_permlane32_swap(d.x, d.z, false, false), v = __builtin_amdgcn_permlane32_swap(d.y, d.w, false, false);
+            const v2u u = __builtin_amdgcn_permlane32_swap(d[t].x, d[t].z, false, false), v = __builtin_amdgcn_permlane32_swap(d[t].y, d[t].w, false, false);
             wv[t][0] = expand_in_order<T>(u.x, mask, base);
             wv[t][1] = expand_in_order<T>(v.x, mask, base);
             wv[t][2] = expand_in_order<T>(u.y, mask, base);
             wv[t][3] = expand_in_order<T>(v.y, mask, base);
         }
+    };
+    auto multiply = [&](auto second) {
+        constexpr bool kSecond = decltype(second)::value;
         for (int t = 0; t < 2; ++t)
             for (int p = 0; p < PIECES; ++p)
                 for (int i = 0; i < 2; ++i) {
@@ -166,31 +169,61 @@ __global__ __launch_bounds__(kThreads, 2) void gated_prompt(LinearW4Args a, Fast
                         for (int e = 0; e < 16; ++e) acc[i][t][e] = fmaf(sc[t][p], sum[e], acc[i][t][e]);
                 }
     };
+    // No more than so many loads under way, and LDS done with; LDS alone.  (Instructions that the compiler counts with, and a line that nothing
+    // in memory crosses.)
+    auto wait_for = [](auto loads) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(decltype(loads)::value | 0x70);
+        asm volatile("" ::: "memory");
+    };
+    auto wait_lds = [] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+        asm volatile("" ::: "memory");
+    };
     for (int g0 = 0; g0 < a.groups; g0 += kGroups) {
         const int n_groups = min(kGroups, a.groups - g0), first = g0 * a.group, last = (int)min((int64_t)first + (int64_t)n_groups * a.group, (int64_t)a.K);
         const int blocks = (last - first + kBlock - 1) / kBlock;
         __syncthreads();
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(scalar_rsrc(w, 4), (__attribute__((address_space(3))) void *)lds.unread, 4, 0, 0, 0, 0);
-        fetch_w(first, w0);
-        // The second term: eight groups' sums of the rows in the place of a step of x, 32 groups at a time.
+        // The second term, sixteen groups at a time: their sums in the places of a step's x and a block's weights that are not needed yet, eight
+        // groups to a row of 128 bytes.
         for (int q0 = 0; q0 < n_groups; q0 += 32) {
-            if (q0 > 0) __syncthreads();
-            // (by registers: a direct load here would have the compiler wait for all of them in the loop below)
-            v4u in[8];
+            v4u in[8];                           // of 32 groups
             for (int i = 0; i < 8; ++i) {
                 const int r = x_row + 64 * (i & 1), g = g0 + q0 + 8 * (i >> 1) + x_piece;
                 in[i] = ((const v4u *)a.sums)[(int64_t)min(m0 + r, a.M - 1) * a.groups + min(g, a.groups - 1)];
                 if (g >= a.groups) in[i] = v4u{0, 0, 0, 0};
             }
-            for (int i = 0; i < 8; ++i) *(v4u *)((i < 2 ? x0 : i < 4 ? x1 : i < 6 ? x2 : x3) + (i & 1) * 8192 + threadIdx.x * 16) = in[i];
-            // and a thread brings sixteen scales and zero points of a column to LDS
-            const int c = threadIdx.x >> 1;
+            // a thread brings sixteen scales and zero points of a column to LDS
+            const int c = threadIdx.x >> 1, g1 = q0 + 16 * (threadIdx.x & 1);
             const int64_t row = row_of(c) * a.groups + g0;
-            const int g1 = q0 + 16 * (threadIdx.x & 1);
-            for (int e = 0; e < 16; ++e) scale[c][g1 + e] = ((const E *)a.scales)[row + min(g1 + e, n_groups - 1)];
-            if (ZEROS)
-                for (int e = 0; e < 16; ++e) zero[c][g1 + e] = a.zeros[row + min(g1 + e, n_groups - 1)];
-            __syncthreads();
+            if (q0 + 32 <= n_groups) {
+                typedef uint32_t at2 __attribute__((ext_vector_type(4), aligned(2)));
+                typedef uint32_t at1 __attribute__((ext_vector_type(4), aligned(1)));
+                const v4u lo = *(const at2 *)((const E *)a.scales + row + g1), hi = *(const at2 *)((const E *)a.scales + row + g1 + 8);
+                v4u z{0, 0, 0, 0};
+                if (ZEROS) z = *(const at1 *)(a.zeros + row + g1);
+                for (int e = 0; e < 4; ++e) {
+                    ((uint32_t *)&scale[c][g1])[e] = lo[e];
+                    ((uint32_t *)&scale[c][g1])[4 + e] = hi[e];
+                    if (ZEROS) ((uint32_t *)&zero[c][g1])[e] = z[e];
+                }
+            } else {
+                for (int e = 0; e < 16; ++e) scale[c][g1 + e] = ((const E *)a.scales)[row + min(g1 + e, n_groups - 1)];
+                if (ZEROS)
+                    for (int e = 0; e < 16; ++e) zero[c][g1 + e] = a.zeros[row + min(g1 + e, n_groups - 1)];
+            }
+            auto bring = [&](const v4u *sums) {
+                for (int i = 0; i < 4; ++i) *(v4u *)((i < 2 ? x3 : w1) + (i & 1) * 8192 + threadIdx.x * 16) = sums[i];
+            };
+            bring(in);
+            if (q0 == 0) {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(scalar_rsrc(w, 4), (__attribute__((address_space(3))) void *)lds.unread, 4, 0, 0, 0, 0);
+                fetch_w(first, w0);
+                fetch_x(first, x0);
+                fetch_x(first + kStep, x1);
+                fetch_x(first + kBlock, x2);
+            }
             auto subtract = [&](int g1, const char *from) {
                 for (int q = 0; q < 4; ++q) {
                     const int g = g1 + 2 * q + half;
@@ -204,38 +237,53 @@ __global__ __launch_bounds__(kThreads, 2) void gated_prompt(LinearW4Args a, Fast
                         for (int t = 0; t < 2; ++t) acc[i][t] = BF16::mfma32(xs[i], ws[t], acc[i][t]);
                 }
             };
-            subtract(q0, x0);
-            if (q0 + 8 < n_groups) subtract(q0 + 8, x1);
-            if (q0 + 16 < n_groups) subtract(q0 + 16, x2);
-            if (q0 + 24 < n_groups) subtract(q0 + 24, x3);
+            for (int s = 0; s < 32 && q0 + s < n_groups; s += 16) {
+                if (s > 0) bring(in + 4);
+                wait_lds();
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                subtract(q0 + s, x3);
+                if (q0 + s + 8 < n_groups) subtract(q0 + s + 8, w1);
+                wait_lds();
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
         }
-        __syncthreads();
-        fetch_x(first, x0);
-        fetch_x(first + kStep, x1);
-        fetch_x(first + kBlock, x2);
-        asm volatile("s_waitcnt vmcnt(4)" ::: "memory");      // (w0: the loads counted below are the only ones under way)
-        // Steps of 64 inputs, x three steps ahead and the weights of a block two: what a step needs has landed when no more than the loads behind
-        // it are under way, and what is fetched takes the place of what all waves have left behind.  (Past the end zeros are fetched: with
-        // loads in a branch the compiler would wait for all of them.)
+        wait_for(std::integral_constant<int, 4>());
+        __builtin_amdgcn_s_barrier();            // (w0 and x0 have landed)
+        asm volatile("" ::: "memory");
+        // Steps of 64 inputs, x three steps ahead and the weights of a block two.  The two waves of a SIMD take turns, half a step apart: while
+        // one reads and expands its operands the other multiplies.  Before the second barrier of a step a wave's loads for the next one have
+        // landed: no more than those behind them are under way.  What is fetched takes the place of what all waves have read.  (Past the end
+        // zeros are fetched: with loads in a branch the compiler would wait for all of them.)
         auto turn = [&](auto allowed, auto second, int k, const char *xs, const char *ws, char *x_to, char *w_to) {
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(allowed)::value) : "memory");
             __builtin_amdgcn_s_barrier();        // (__syncthreads would wait for all loads)
             asm volatile("" ::: "memory");
             if (!decltype(second)::value) fetch_w(k + kBlock, w_to);
             fetch_x(k + 3 * kStep, x_to);
             __builtin_amdgcn_sched_barrier(0);   // (else they are put off to the products' end)
-            use(second, k, g0, xs, ws);
+            read(second, k, g0, xs, ws);
+            __builtin_amdgcn_sched_barrier(0);
+            wait_for(allowed);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_setprio(1);
+            multiply(second);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
         };
         typedef std::integral_constant<int, 4> Four;
         typedef std::integral_constant<int, 6> Six;
+        if (wave >= 4) __builtin_amdgcn_s_barrier();
         for (int k = first; k < last; k += 2 * kBlock) {
-            turn(Four(), std::false_type(), k, x0, w0, x3, w1);
-            turn(Six(), std::true_type(), k + kStep, x1, w0, x0, nullptr);
+            turn(Six(), std::false_type(), k, x0, w0, x3, w1);
+            turn(Four(), std::true_type(), k + kStep, x1, w0, x0, nullptr);
             if (k + kBlock >= last) break;
-            turn(Four(), std::false_type(), k + kBlock, x2, w1, x1, w0);
-            turn(Six(), std::true_type(), k + kBlock + kStep, x3, w1, x2, nullptr);
+            turn(Six(), std::false_type(), k + kBlock, x2, w1, x1, w0);
+            turn(Four(), std::true_type(), k + kBlock + kStep, x3, w1, x2, nullptr);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (wave < 4) __builtin_amdgcn_s_barrier();
+        wait_for(std::integral_constant<int, 0>());
     }
 
     const bool inside = n0 + wn + col < a.N;
