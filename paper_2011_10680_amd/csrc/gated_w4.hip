@@ -314,18 +314,73 @@ __global__ __launch_bounds__(kThreads, 2) void gated_prompt(LinearW4Args a, Fast
     }
 }
 
-template <class T>
-bool whole_rows(const LinearW4Args &a) { return ((uintptr_t)a.x & 15) == 0 && a.x_stride % 8 == 0 && a.K % 32 == 0 && ((uintptr_t)a.w & 15) == 0; }
+// Time of a form in us: `at` for the launch, `in` for every 4096 inputs of the first workgroups, one to each of the 256 compute units, and `more` and
+// `begin` for every 256 after them.  Fitted to 150 calls of 1 to 800 rows, 512 to 16384 outputs and 256 to 11008 inputs, in groups of 128
+// (off by a sixteenth at the median): the form chosen by it took 1.02 times the best one's time in the mean, 1.2 times at most.  Larger forms
+// begin whole rounds, small ones share a unit.
+struct Form { int rows, outputs; float at, in, more, begin; bool rounds; };
+constexpr Form kForms[] = {{16, 16, 5.6f, 3.6f, 6.1f, 1.2f, false}, {16, 32, 7.9f, 5.9f, 10.1f, 3.2f, false}, {32, 16, 6.2f, 5.8f, 8.6f, 1.0f, false},
+                           {32, 32, 9.1f, 8.0f, 13.3f, 4.0f, true}, {64, 32, 11.1f, 11.9f, 21.6f, 4.4f, true}};
+constexpr Form kPrompt = {kRows, kOuts, 13.2f, 46.9f, 49.7f, 12.0f, true};
+constexpr float kScaledTwice = 1.25f, kScaledFour = 1.6f;      // groups of 64 and 32 (8192 x 4096, 256 rows: 63, 74 and 99 us)
+float time_of(const Form &f, const LinearW4Args &a) {
+    const int64_t blocks = ((int64_t)a.N + f.outputs - 1) / f.outputs * (((int64_t)a.M + f.rows - 1) / f.rows);
+    const float k = (float)a.K / 4096.f, rounds = f.rounds ? (float)((blocks + 255) / 256) : (float)blocks / 256.f;
+    return f.at + f.in * k + (rounds > 1 ? rounds - 1 : 0.f) * (f.more * k + f.begin);
+}
+// the best of the forms whose bit is set; up to 16 rows the first (one row of 12288 outputs 16.5 us, the second 22.4)
+int best_form(const LinearW4Args &a, unsigned forms) {
+    int best = 0;
+    if (a.M > 16)
+        for (int i = 1; i < 5; ++i)
+            if ((forms >> i & 1) && time_of(kForms[i], a) < time_of(kForms[best], a)) best = i;
+    return best;
+}
 
-bool prompt_sized(const LinearW4Args &a) { return a.M > 128 && a.K <= kMostInputs && a.x_stride <= kMostXStride && a.K % 32 == 0 && a.x_stride % 8 == 0; }
+template <class T, int PIECES, int ALIGN>
+hawq_status pick_tiles(const LinearW4Args &a, hipStream_t s) {
+    const int best = best_form(a, ALIGN == 16 ? 0x1f : 0x05);
+    if constexpr (ALIGN == 16) {
+        if (best == 1) return launch<T, 4, 1, PIECES, ALIGN, true>(a, s);
+        if (best == 3) return launch<T, 4, 2, PIECES, ALIGN, true>(a, s);
+        if (best == 4) return launch<T, 4, 4, PIECES, ALIGN, true>(a, s);
+    }
+    return best == 2 ? launch<T, 2, 2, PIECES, ALIGN, true>(a, s) : launch<T, 2, 1, PIECES, ALIGN, true>(a, s);
+}
+
+template <class T, int ALIGN>
+hawq_status pick_pieces(const LinearW4Args &a, hipStream_t s) {
+    return a.group % 128 == 0 ? pick_tiles<T, 1, ALIGN>(a, s) : a.group % 64 == 0 ? pick_tiles<T, 2, ALIGN>(a, s) : pick_tiles<T, 4, ALIGN>(a, s);
+}
 
 template <class T>
-hawq_status launch_prompt(const LinearW4Args &a, hipStream_t s) {
+hawq_status few_rows(const LinearW4Args &a, hipStream_t s) {
+    const bool x16 = ((uintptr_t)a.x & 15) == 0 && a.x_stride % 8 == 0 && a.x_stride < (1 << 25);      // (32-bit offsets inside 64 rows)
+    if (x16 && a.K % 32 == 0 && ((uintptr_t)a.w & 15) == 0) return pick_pieces<T, 16>(a, s);
+    if (x16 && a.K % 8 == 0 && ((uintptr_t)a.w & 3) == 0) return pick_pieces<T, 4>(a, s);
+    return pick_pieces<T, 1>(a, s);
+}
+
+// What the prompt kernel takes by its sizes (the workspace goes by them alone), and by its addresses.
+bool prompt_sized(const LinearW4Args &a) {
+    if (a.M <= 16 || a.K > kMostInputs || a.x_stride > kMostXStride || a.K % 32 != 0 || a.x_stride % 8 != 0) return false;
+    const float more = a.group % 128 == 0 ? 1.f : a.group % 64 == 0 ? kScaledTwice : kScaledFour;
+    return more * time_of(kPrompt, a) < time_of(kForms[best_form(a, 0x1f)], a);
+}
+bool prompt_placed(const LinearW4Args &a) { return ((uintptr_t)a.x & 15) == 0 && ((uintptr_t)a.w & 15) == 0; }
+
+template <class T>
+hawq_status prompt(const LinearW4Args &all, hipStream_t s) {
+    LinearW4Args a = all;
+    // Rows past the last whole tile, up to 16, go by the form for few where their tiles would begin another round of the 256 compute units.
+    const int64_t n_tiles = ((int64_t)a.N + kOuts - 1) / kOuts, rest = a.M % kRows;
+    const auto rounds = [&](int64_t m_tiles) { return (m_tiles * n_tiles + 255) / 256; };
+    if (rest > 0 && rest <= 16 && rounds(a.M / kRows + 1) > rounds(a.M / kRows)) a.M -= (int32_t)rest;
     const Grid rows = spread(a.M, 1, 256);
     group_sums<T><<<dim3((unsigned)rows.x, (unsigned)rows.y), 256, 0, s>>>(a);
     hawq_status st = check_launch();
     if (st != HAWQ_OK) return st;
-    const int64_t m_tiles = ((int64_t)a.M + kRows - 1) / kRows, n_tiles = ((int64_t)a.N + kOuts - 1) / kOuts, at_once = most_blocks(kThreads) / m_tiles;
+    const int64_t m_tiles = ((int64_t)a.M + kRows - 1) / kRows, at_once = most_blocks(kThreads) / m_tiles;
     const FastDiv by_group = fast_div((uint32_t)a.group);
     for (int64_t n = 0; n < n_tiles; n += at_once) {                     // as many outputs as a launch holds
         const int tiles = (int)(m_tiles * (n_tiles - n < at_once ? n_tiles - n : at_once)), first_n = (int)n * kOuts;
@@ -340,32 +395,21 @@ hawq_status launch_prompt(const LinearW4Args &a, hipStream_t s) {
         st = check_launch();
         if (st != HAWQ_OK) return st;
     }
-    return HAWQ_OK;
-}
-
-template <class T, int PIECES, int ALIGN>
-hawq_status pick_tiles(const LinearW4Args &a, hipStream_t s) {
-    return a.M > 16 ? launch<T, 2, 2, PIECES, ALIGN, true>(a, s) : launch<T, 2, 1, PIECES, ALIGN, true>(a, s);
-}
-
-template <class T, int ALIGN>
-hawq_status pick_pieces(const LinearW4Args &a, hipStream_t s) {
-    return a.group % 128 == 0 ? pick_tiles<T, 1, ALIGN>(a, s) : a.group % 64 == 0 ? pick_tiles<T, 2, ALIGN>(a, s) : pick_tiles<T, 4, ALIGN>(a, s);
-}
-
-template <class T>
-hawq_status pick_align(const LinearW4Args &a, hipStream_t s) {
-    if (prompt_sized(a) && whole_rows<T>(a)) return launch_prompt<T>(a, s);
-    const bool x16 = ((uintptr_t)a.x & 15) == 0 && a.x_stride % 8 == 0 && a.x_stride < (1 << 25);      // (32-bit offsets inside 64 rows)
-    if (x16 && a.K % 32 == 0 && ((uintptr_t)a.w & 15) == 0) return pick_pieces<T, 16>(a, s);
-    if (x16 && a.K % 8 == 0 && ((uintptr_t)a.w & 3) == 0) return pick_pieces<T, 4>(a, s);
-    return pick_pieces<T, 1>(a, s);
+    if (a.M == all.M) return HAWQ_OK;
+    LinearW4Args last = all;
+    last.M = all.M - a.M;
+    last.x = (const uint16_t *)all.x + (int64_t)a.M * a.x_stride;
+    last.y = (uint16_t *)all.y + (int64_t)a.M * a.y_stride;
+    return few_rows<T>(last, s);
 }
 
 }  // namespace
 
 size_t gated_w4_workspace(const LinearW4Args &a) { return prompt_sized(a) ? (size_t)a.M * a.groups * 16 : 0; }
 
-hawq_status launch_gated_w4(const LinearW4Args &a, hipStream_t s) { return a.dtype == HAWQ_F16 ? pick_align<F16>(a, s) : pick_align<BF16>(a, s); }
+hawq_status launch_gated_w4(const LinearW4Args &a, hipStream_t s) {
+    if (prompt_sized(a) && prompt_placed(a)) return a.dtype == HAWQ_F16 ? prompt<F16>(a, s) : prompt<BF16>(a, s);
+    return a.dtype == HAWQ_F16 ? few_rows<F16>(a, s) : few_rows<BF16>(a, s);
+}
 
 }  // namespace hawq

@@ -7,7 +7,7 @@ import lm_step_reference as ref
 pytestmark = pytest.mark.gpu
 
 
-def _run(M, N, K, group, dtype, zeros, bias, kind="silu", x_pad=0, y_pad=0, w_at=0, x_at=0, mean=0.0, seed=0):
+def _run(M, N, K, group, dtype, zeros, bias, kind="silu", x_pad=0, y_pad=0, w_at=0, x_at=0, mean=0.0, prompt=None, seed=0):
     import torch
     import paper_2011_10680_amd as hawq
     dt = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype]
@@ -30,6 +30,7 @@ def _run(M, N, K, group, dtype, zeros, bias, kind="silu", x_pad=0, y_pad=0, w_at
     d = hawq.GatedW4Desc(M=M, N=N, K=K, group=group, x_dtype=hawq.F16 if dtype == "f16" else hawq.BF16, w_dtype=hawq.U4 if zeros else hawq.S4,
                          activation={"silu": hawq.SILU, "gelu": hawq.GELU, "gelu_tanh": hawq.GELU_TANH, "relu": hawq.RELU}[kind], x_stride=K + x_pad, y_stride=N + y_pad)
     room = hawq.hawq_gated_w4_workspace_bytes(d)
+    assert prompt is None or (room > 0) == prompt          # the kernel for whole prompts has a workspace
     workspace = torch.full((room + 256,), 0xFF, dtype=torch.uint8, device="cuda")      # (not-a-number in 32 bits)
     hawq.hawq_gated_w4(d, xd, wd, s.cuda(), None if z is None else torch.from_numpy(z).cuda(), None if b is None else b.cuda(), y, workspace[:room] if room else None)
     torch.cuda.synchronize()
@@ -78,17 +79,29 @@ def test_strides_and_alignment(x_pad, x_at, w_at):
         _run(M, 70, 328, 64, "bf16", False, True, x_pad=x_pad, x_at=x_at, w_at=w_at)
 
 
+@pytest.mark.parametrize("M,N,K,group", [(400, 5000, 32, 32), (257, 5001, 64, 64), (200, 9000, 96, 32), (200, 5000, 128, 128), (400, 5000, 288, 96), (400, 3000, 352, 64), (1040, 2113, 160, 8224),
+                                         (300, 3000, 512, 128), (529, 3001, 1056, 96), (800, 2000, 1120, 32), (257, 5000, 4160, 32), (257, 5000, 8320, 64), (257, 5100, 1024, 256)])
+def test_whole_prompts(M, N, K, group):
+    """Tiles that end inside, steps that end inside, more groups than are in LDS at once, rows past the last whole tile (1, 16, 17 of them)."""
+    for i, dtype in enumerate(("bf16", "f16")):
+        _run(M + 15 * i, N, K, group, dtype, i == 0, i == 1, x_pad=8 * i, y_pad=3 * i, w_at=16 * i, prompt=True, seed=K)
+
+
+@pytest.mark.parametrize("kind", ["gelu", "gelu_tanh", "relu"])
+def test_whole_prompts_activations(kind):
+    _run(300, 3000, 512, 128, "f16", False, True, kind, prompt=True, seed=5)
+
+
 @pytest.mark.parametrize("M,N,K", [(3, 40, 20000), (20, 6200, 4160), (300, 500, 4160)])
 def test_many_groups(M, N, K):
     _run(M, N, K, 32, "bf16", True, False, seed=K)
 
 
-@pytest.mark.parametrize("M", [2, 140])
-def test_infinities_and_no_numbers(M):
+@pytest.mark.parametrize("M,N,K", [(2, 40, 256), (140, 40, 256), (300, 5000, 512)])
+def test_infinities_and_no_numbers(M, N, K):
     """An infinite input shows in its own row alone: as the formula has it, an infinity or no number."""
     import torch
     import paper_2011_10680_amd as hawq
-    N, K = 40, 256
     g = torch.Generator(device="cuda").manual_seed(1)
     x = torch.randn((M, K), generator=g, device="cuda").half()
     x[1, 5], x[M - 1, 7] = float("inf"), float("nan")
@@ -108,12 +121,12 @@ def test_infinities_and_no_numbers(M):
     assert (got[~fine & ~np.isnan(want)] == want[~fine & ~np.isnan(want)]).all()
 
 
-@pytest.mark.parametrize("M", [1, 200])
-def test_one_row_for_all(M):
+@pytest.mark.parametrize("M,N", [(1, 48), (200, 48), (300, 9000)])
+def test_one_row_for_all(M, N):
     """x_stride 0: every row of y is the same."""
     import torch
     import paper_2011_10680_amd as hawq
-    N, K = 48, 128
+    K = 128
     g = torch.Generator(device="cuda").manual_seed(2)
     x = torch.randn((1, K), generator=g, device="cuda").bfloat16()
     w = torch.randint(0, 256, (2 * N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
