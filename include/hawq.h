@@ -610,6 +610,7 @@ hawq_status hawq_adapters(const hawq_adapters_desc *desc, const void *x, const v
  * (a number outside 0..n_allowed - 1, as -1: everything is allowed); allowed_row == NULL: row t's is the t-th, n_allowed >= total.  A mask
  * may leave a row empty: all of it is -infinity then.  n_bias == 0 and n_allowed == 0: none, their pointers are not looked at.
  * y may be x, with its stride (HAWQ_ERR_SHAPE otherwise); only what changes is then written.  No other overlap.
+ * Fewer than 2^23 rows, and a past_stride below that; up to 2^31 - 4096 tokens in the vocabulary.
  */
 typedef struct {
     int32_t n_seqs, total, vocab;

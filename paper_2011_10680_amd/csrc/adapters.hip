@@ -264,7 +264,7 @@ Plan plan(const AdaptersArgs &a) {
     p.mt = a.M >= 512 ? 4 : 1;
     const int64_t tiles = ((int64_t)a.M + 16 * p.mt - 1) / (16 * p.mt), steps = ((int64_t)a.K + 4 * kSteps - 1) / (4 * kSteps);
     p.slots = p.mt == 4 ? 1 : a.n_adapters < 16 ? (a.n_adapters > 0 ? a.n_adapters : 1) : 16;
-    const int64_t wanted = (p.mt == 4 ? 256 : 512) / (tiles * (p.slots < 4 ? p.slots : 4)), most = steps < 16 ? steps : 16;
+    const int64_t wanted = 512 / (tiles * (p.slots < 4 ? p.slots : 4)), most = steps < 16 ? steps : 16;
     p.splits = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
     return p;
 }

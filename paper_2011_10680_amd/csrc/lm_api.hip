@@ -278,6 +278,7 @@ hawq_status hawq_logits(const hawq_logits_desc *d, const void *x, const int32_t 
     if (!starts && d->total != d->n_seqs) return HAWQ_ERR_SHAPE;
     if (d->n_allowed > 0 && !allowed_row && d->n_allowed < d->total) return HAWQ_ERR_SHAPE;
     if (d->n_seqs == 0 || d->total == 0) return HAWQ_OK;
+    if (d->total >= (1 << 23) || d->past_stride >= (1 << 23) || d->vocab > kMostRows) return HAWQ_ERR_UNSUPPORTED;      // (a token is counted in 24 bits)
     if (!x || !y || (penalties && d->past_stride > 0 && (!past || !past_lens)) || (d->n_bias > 0 && (!bias_starts || !bias_ids || !bias_values)) ||
         (d->n_allowed > 0 && !allowed))
         return HAWQ_ERR_NULL;

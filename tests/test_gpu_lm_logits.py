@@ -84,6 +84,13 @@ def test_requests(drafts):
         _run(drafts, 600, [13 * j % 50 for j in range(len(drafts))], "bf16" if i % 2 else "f16", biases=6, masks=4, use=use, few=40, seed=i)
 
 
+@pytest.mark.parametrize("n", [63, 64, 65, 200, 4096, 4097, 5000])
+def test_many_requests(n):
+    """A row's request is found among all, empty ones and rows behind the last one too."""
+    r = np.random.default_rng(n)
+    _run(r.integers(0, 3, size=n).tolist() + [1], 40, r.integers(0, 6, size=n + 1).tolist(), "bf16", biases=1, masks=3, behind=2, few=40, seed=n)
+
+
 def test_one_row_each_without_starts():
     for drafts in (True, False):
         _run([1] * 7, 900, [4, 0, 9, 100, 1, 2, 50], "f16", biases=3, masks=7, use=("prompt", "penalties") + (("drafts",) if drafts else ()), seed=1)
@@ -136,6 +143,17 @@ def test_the_same_token_twice_in_a_list_has_its_last_value():
     def change(i):
         i["bias_ids"][:] = 5
     _run([1, 2, 1], 700, [4, 4, 4], "f16", biases=40, few=9, seed=5, change=change)
+
+
+@pytest.mark.parametrize("V", [30, 1000, 8193, 20001])
+def test_long_lists_of_biases(V):
+    """Lists longer than are searched for every token, with tokens listed more than once, and short ones beside them."""
+    def change(i):
+        n = i["bias_starts"]
+        n[:] = np.concatenate(([0], np.sort(np.random.default_rng(1).integers(0, n[-1], size=len(n) - 2)), [n[-1]]))
+    for in_place in (False, True):
+        _run([2, 1, 3], V, [50, 3, 200], "f16", biases=3000, masks=3, in_place=in_place, pad=3, few=V + 1, seed=V, change=change)
+        _run([1, 1], V, [5, 30], "bf16", biases=66, y_pad=5, seed=V)
 
 
 def test_masked_values_whatever_they_hold():
