@@ -18,6 +18,9 @@ namespace hawq {
 namespace {
 
 constexpr int kSteps = 64;                       // k of a step
+// Waves that share K out in a workgroup of the inner product: more leave fewer parts to add up (48 rows over twelve adapters 15.1 us with 8, 16.9
+// with 4), and a wave of 64 rows has registers for few beside it (5003 rows: 69 and 60).
+constexpr int waves_of(int mt) { return mt == 1 ? 8 : 4; }
 constexpr int kRanks = 128;                      // ranks of the outer product that are staged at once
 
 struct Plan {
@@ -113,18 +116,18 @@ __device__ __forceinline__ void inner_tile(const AdaptersArgs &a, int m0, int id
         __syncthreads();
         for (int t = 0; t < NT; ++t) *(v4f *)(red + (wave * 16 + r) * kRow + 16 * t + 4 * c) = acc[i][t];
         __syncthreads();
-        for (int e = threadIdx.x; e < 256 * NT; e += 256) {
+        for (int e = threadIdx.x; e < 256 * NT; e += 64 * waves_of(MT)) {
             const int m = e / (16 * NT), j = e % (16 * NT);
             float v = 0;
-            for (int w = 0; w < 4; ++w) v += red[(w * 16 + m) * kRow + j];
+            for (int w = 0; w < waves_of(MT); ++w) v += red[(w * 16 + m) * kRow + j];
             if ((rows >> (16 * i + m) & 1) && rb + j < rank) h[(int64_t)(m0 + 16 * i + m) * a.max_rank + rb + j] = v;
         }
     }
 }
 
 template <class T, int MT, bool VECTOR>
-__global__ __launch_bounds__(256) void inner(AdaptersArgs a, int slots, int splits) {
-    __shared__ __align__(16) float red[4 * 16 * 68];
+__global__ __launch_bounds__(64 * waves_of(MT)) void inner(AdaptersArgs a, int slots, int splits) {
+    __shared__ __align__(16) float red[waves_of(MT) * 16 * 68];
     const int64_t tile = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (tile * (16 * MT) >= a.M) return;
     const int m0 = (int)tile * (16 * MT), slot = blockIdx.z % slots, split = blockIdx.z / slots;
@@ -132,9 +135,9 @@ __global__ __launch_bounds__(256) void inner(AdaptersArgs a, int slots, int spli
     each_adapter<MT>(a, m0, slot, slots, false, [&](int id, int rank, uint64_t rows) {
         for (int rb = 0; rb < rank; rb += 64) {
             const int tiles = (rank - rb + 15) / 16;
-            if (tiles == 1) inner_tile<T, MT, 1, VECTOR>(a, m0, id, rank, rb, rows, 4 * split, 4 * splits, h, red);
-            else if (tiles == 2) inner_tile<T, MT, 2, VECTOR>(a, m0, id, rank, rb, rows, 4 * split, 4 * splits, h, red);
-            else inner_tile<T, MT, 4, VECTOR>(a, m0, id, rank, rb, rows, 4 * split, 4 * splits, h, red);
+            if (tiles == 1) inner_tile<T, MT, 1, VECTOR>(a, m0, id, rank, rb, rows, waves_of(MT) * split, waves_of(MT) * splits, h, red);
+            else if (tiles == 2) inner_tile<T, MT, 2, VECTOR>(a, m0, id, rank, rb, rows, waves_of(MT) * split, waves_of(MT) * splits, h, red);
+            else inner_tile<T, MT, 4, VECTOR>(a, m0, id, rank, rb, rows, waves_of(MT) * split, waves_of(MT) * splits, h, red);
         }
     });
 }
@@ -189,6 +192,12 @@ __global__ __launch_bounds__(256) void outer(AdaptersArgs a, int slots, int spli
         const E *b = (const E *)a.b + (int64_t)max(id, 0) * a.b_adapter;
         for (int p = 0; p < passes; ++p) {
             const int n0 = ((chunk * passes + p) * 4 + wave) * 64;
+            const int n = n0 + 16 * c;
+            typename T::v8 ahead[ROWS ? MT : 1][2];      // base, on its way under the products
+            if (ROWS)
+                for (int i = 0; i < MT; ++i)
+                    for (int q = 0; q < 2; ++q)
+                        if (n + 16 <= a.N && (rows >> (16 * i + r) & 1)) ahead[i][q] = *(const typename T::v8 *)((const E *)a.base + (m0 + 16 * i + r) * a.base_stride + n + 8 * q);
             v4f acc[MT][4];
             for (int i = 0; i < MT; ++i)
                 for (int t = 0; t < 4; ++t) acc[i][t] = v4f{0, 0, 0, 0};
@@ -231,7 +240,6 @@ __global__ __launch_bounds__(256) void outer(AdaptersArgs a, int slots, int spli
                         }
                 }
             }
-            const int n = n0 + 16 * c;
             if (n >= a.N) continue;
             for (int i = 0; i < MT; ++i) {
                 const int m = m0 + 16 * i + r;
@@ -242,7 +250,7 @@ __global__ __launch_bounds__(256) void outer(AdaptersArgs a, int slots, int spli
                 auto sum = [&](E v, float add) { return id >= 0 ? (E)((float)v + scale * add * up) : v; };
                 if (ROWS && n + 16 <= a.N) {
                     for (int q = 0; q < 2; ++q) {
-                        typename T::v8 v = *(const typename T::v8 *)(base + 8 * q);
+                        typename T::v8 v = ahead[ROWS ? i : 0][q];
                         for (int e = 0; e < 8; ++e) v[e] = sum(v[e], acc[i][2 * q + (e >> 2)][e & 3]);
                         *(typename T::v8 *)(y + 8 * q) = v;
                     }
@@ -261,10 +269,13 @@ __global__ __launch_bounds__(256) void outer(AdaptersArgs a, int slots, int spli
 
 Plan plan(const AdaptersArgs &a) {
     Plan p;
-    p.mt = a.M >= 512 ? 4 : 1;
-    const int64_t tiles = ((int64_t)a.M + 16 * p.mt - 1) / (16 * p.mt), steps = ((int64_t)a.K + 4 * kSteps - 1) / (4 * kSteps);
+    // A tile of 64 rows reads an adapter a fourth as often and is taken once for all that occur in it, one of 16 has more beside it (4096 x 4096,
+    // us, 16 and 64 rows: one adapter of rank 64 at a time 29 and 43 for 600 rows, 56 and 60 for 2500, 89 and 70 for 5000; of rank 16 mixed
+    // 48 and 75, 85 and 95)
+    p.mt = a.M >= 4096 ? 4 : 1;
+    const int64_t tiles = ((int64_t)a.M + 16 * p.mt - 1) / (16 * p.mt), each = waves_of(p.mt) * kSteps, steps = (a.K + each - 1) / each;
     p.slots = p.mt == 4 ? 1 : a.n_adapters < 16 ? (a.n_adapters > 0 ? a.n_adapters : 1) : 16;
-    const int64_t wanted = 512 / (tiles * (p.slots < 4 ? p.slots : 4)), most = steps < 16 ? steps : 16;
+    const int64_t wanted = (p.mt == 1 ? 256 : 512) / (tiles * (p.slots < 4 ? p.slots : 4)), most = steps < 16 ? steps : 16;
     p.splits = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
     return p;
 }
@@ -274,11 +285,11 @@ hawq_status launch(const AdaptersArgs &a, const Plan &p, hipStream_t s) {
     const int64_t tiles = ((int64_t)a.M + 16 * MT - 1) / (16 * MT);
     const auto eights = [](int64_t strides, uintptr_t pointers) { return strides % 8 == 0 && pointers % 16 == 0; };
     if (a.n_adapters > 0) {
-        const Grid g = spread(tiles, 1, 256);
+        const Grid g = spread(tiles, 1, 64 * waves_of(MT));
         if (g.x == 0) return HAWQ_ERR_UNSUPPORTED;
         const dim3 grid((unsigned)g.x, (unsigned)g.y, (unsigned)(p.slots * p.splits));
-        if (eights(a.K | a.x_stride | a.a_adapter | a.a_row, (uintptr_t)a.x | (uintptr_t)a.a)) inner<T, MT, true><<<grid, 256, 0, s>>>(a, p.slots, p.splits);
-        else inner<T, MT, false><<<grid, 256, 0, s>>>(a, p.slots, p.splits);
+        if (eights(a.K | a.x_stride | a.a_adapter | a.a_row, (uintptr_t)a.x | (uintptr_t)a.a)) inner<T, MT, true><<<grid, 64 * waves_of(MT), 0, s>>>(a, p.slots, p.splits);
+        else inner<T, MT, false><<<grid, 64 * waves_of(MT), 0, s>>>(a, p.slots, p.splits);
         const hawq_status st = check_launch();
         if (st != HAWQ_OK) return st;
     }

@@ -87,7 +87,8 @@ def test_many_adapters_in_any_order_and_none():
     _run(1000, 32, 64, 2, 16, "bf16", adapter=[(i // 3) % 3 - 1 for i in range(1000)])
 
 
-@pytest.mark.parametrize("M,N,K,most", [(512, 300, 64, 64), (577, 33, 200, 8), (640, 1000, 72, 136), (1030, 64, 1000, 20)])
+@pytest.mark.parametrize("M,N,K,most", [(512, 300, 64, 64), (577, 33, 200, 8), (640, 1000, 72, 136), (1030, 64, 1000, 20), (4096, 300, 64, 64), (4097, 33, 200, 8), (4160, 100, 72, 136),
+                                        (4300, 64, 1000, 20)])
 def test_whole_prompts(M, N, K, most):
     """Requests' rows one behind the other, and in between one in no order."""
     for i, dtype in enumerate(("f16", "bf16")):
