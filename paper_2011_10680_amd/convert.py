@@ -213,3 +213,27 @@ def quantize_groups(W, group, zero_points=False, dtype=None):
         q = np.clip(np.rint(g / S[:, :, None]), -W_MAX[4], W_MAX[4])
     q = q.reshape(N, -1)[:, :K].astype(np.int64) & 15
     return (q[:, 0::2] | q[:, 1::2] << 4).astype(np.uint8), S, None if zeros is None else zeros.astype(np.uint8)
+
+
+def rotary_turns(rotary_dim, base=10000.0, scaling="none", factor=1.0, original=None, low=1.0, high=32.0):
+    """Revolutions per token of every pair, float64 [rotary_dim / 2], as hawq_rotary takes them: base^(-2 f / rotary_dim) / (2 pi).
+    scaling, for contexts `factor` times as long as the model learned: "linear": all are divided by the factor; "base": the base grows by
+    factor^(d / (d - 2)), so that the slowest pair is slowed by the factor and the fastest not at all; "parts": pairs that turn fewer than `low`
+    times in the original context are slowed by the factor, those that turn more than `high` times are not, in between a mixture by the number of turns."""
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError("rotary_turns: rotary_dim must be even and positive")
+    if not (base > 0 and factor >= 1):
+        raise ValueError("rotary_turns: base must be positive and factor 1 or more")
+    if scaling == "base":
+        base = base * factor ** (rotary_dim / max(rotary_dim - 2, 1))
+    turns = base ** (-np.arange(0, rotary_dim, 2, dtype=np.float64) / rotary_dim) / (2 * np.pi)
+    if scaling in ("none", "base"):
+        return turns
+    if scaling == "linear":
+        return turns / factor
+    if scaling == "parts":
+        if original is None or not 0 < low < high:
+            raise ValueError("rotary_turns: parts needs the original context and 0 < low < high")
+        kept = np.clip((turns * original - low) / (high - low), 0.0, 1.0)
+        return turns * (kept + (1 - kept) / factor)
+    raise ValueError("rotary_turns: scaling is none, linear, base or parts")

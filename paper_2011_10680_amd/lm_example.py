@@ -5,16 +5,20 @@ of the cache (`hawq_cache_plan`, `hawq_cache_store`).  Then every step drafts a 
 all of them in one pass (`hawq_attn_tree`) and keeps the longest branch that the model itself would have written, so that the answer is
 that of decoding token by token.  The model is random: norms, gates and residuals are plain torch.
 
-    python -m paper_2011_10680_amd.lm_example [--cache s8] [--tokens 24]
+With `whole` the rest of a step runs in the library too: positions (`hawq_rotary`), the feed-forward's gate (`hawq_gated_w4`), adapters of the
+requests' own (`hawq_adapters`), and rules for the answers (`hawq_logits`), which see a drafted token's own branch.
+
+    python -m paper_2011_10680_amd.lm_example [--cache s8] [--tokens 24] [--whole]
 """
 import argparse
 
 import numpy as np
 import torch
 
-from . import (BF16, F16, S4, S8, U4, AttnPromptDesc, AttnTreeDesc, CacheDesc, CacheStoreDesc, LinearW4Desc, hawq_attn_prompt, hawq_attn_tree,
-               hawq_attn_tree_workspace_bytes, hawq_cache_plan, hawq_cache_store, hawq_linear_w4)
-from .convert import quantize_groups
+from . import (BF16, F16, ROTARY_HALVES, S4, S8, SILU, U4, AdaptersDesc, AttnPromptDesc, AttnTreeDesc, CacheDesc, CacheStoreDesc, GatedW4Desc, LinearW4Desc, LogitsDesc,
+               RotaryDesc, hawq_adapters, hawq_adapters_workspace_bytes, hawq_attn_prompt, hawq_attn_tree, hawq_attn_tree_workspace_bytes, hawq_cache_plan, hawq_cache_store,
+               hawq_gated_w4, hawq_gated_w4_workspace_bytes, hawq_linear_w4, hawq_logits, hawq_rotary)
+from .convert import quantize_groups, rotary_turns
 
 CONFIG = dict(layers=2, width=256, hidden=512, q_heads=8, kv_heads=2, head_dim=64, vocab=512, group=64, page=16, pages=256)
 _HAWQ = {torch.float16: F16, torch.bfloat16: BF16}
@@ -40,12 +44,62 @@ class Linear:
         hawq_linear_w4(d, x, self.w, self.scales, self.zeros, None, y)
         return y
 
+    def gated(self, x):
+        """silu of the first half of the outputs times the second half."""
+        N = self.N // 2
+        y = torch.empty((x.shape[0], N), dtype=self.dtype, device=x.device)
+        d = GatedW4Desc(M=x.shape[0], N=N, K=self.K, group=self.group, x_dtype=_HAWQ[self.dtype], w_dtype=S4 if self.zeros is None else U4, activation=SILU,
+                        x_stride=x.stride(0), y_stride=N)
+        room = torch.empty(hawq_gated_w4_workspace_bytes(d), dtype=torch.uint8, device=x.device)
+        hawq_gated_w4(d, x, self.w, self.scales, self.zeros, None, y, room)
+        return y
+
     def real(self):
         """The matrix that the nibbles stand for, for checks."""
         q = torch.stack((self.w & 15, self.w >> 4), dim=2).reshape(self.N, self.K).float()
         spread = lambda t: t.float().repeat_interleave(self.group, dim=1)[:, :self.K]  # noqa: E731
         q = torch.where(q >= 8, q - 16, q) if self.zeros is None else q - spread(self.zeros)
         return q * spread(self.scales)
+
+
+class Adapters:
+    """Low-rank additions to one projection, of different ranks: a [adapter, rank, inputs], b [adapter, outputs, rank]."""
+
+    def __init__(self, r, ranks, N, K, dtype):
+        most = max(ranks)
+        self.a = torch.from_numpy(r.normal(size=(len(ranks), most, K)) / K ** 0.5).to(dtype).cuda()
+        self.b = torch.from_numpy(r.normal(size=(len(ranks), N, most)) / most ** 0.5).to(dtype).cuda()
+        self.ranks, self.scales = torch.tensor(ranks, dtype=torch.int32, device="cuda"), torch.full((len(ranks),), 0.5, device="cuda")
+
+    def add(self, x, y, adapter):
+        """y += what the rows' adapters make of x."""
+        n, most, K = self.a.shape
+        d = AdaptersDesc(M=x.shape[0], N=y.shape[1], K=K, n_adapters=n, max_rank=most, dtype=_HAWQ[x.dtype], x_stride=x.stride(0), base_stride=y.stride(0), y_stride=y.stride(0),
+                         a_adapter=self.a.stride(0), a_row=self.a.stride(1), b_adapter=self.b.stride(0), b_row=self.b.stride(1))
+        room = torch.empty(hawq_adapters_workspace_bytes(d), dtype=torch.uint8, device=x.device)
+        hawq_adapters(d, x, self.a, self.b, self.ranks, self.scales, adapter, y, y, room)
+
+
+class Rules:
+    """What the answers of n requests obey: (repetition, presence, frequency), a bias for some tokens, and the tokens allowed at all (None: all)."""
+
+    def __init__(self, n, vocab, penalties=(1.0, 0.0, 0.0), biases=None, allowed=None):
+        biases = biases or {}
+        self.penalties = torch.tensor([penalties] * n, dtype=torch.float32, device="cuda")
+        self.starts = torch.arange(n + 1, dtype=torch.int32, device="cuda") * len(biases)
+        self.ids = torch.tensor(list(biases) * n, dtype=torch.int32, device="cuda")
+        self.values = torch.tensor(list(biases.values()) * n, dtype=torch.float32, device="cuda")
+        bits = np.zeros((1, -(-vocab // 32)), np.uint32)
+        for v in allowed if allowed is not None else ():
+            bits[0, v // 32] |= np.uint32(1 << v % 32)
+        self.allowed = None if allowed is None else torch.from_numpy(bits.view(np.int32)).cuda()
+
+    def apply(self, logits, past, past_lens, prompt_lens, starts=None, drafts=None, mask=None):
+        """In place; one row for each request, or rows packed by starts, each behind its own branch of the drafts."""
+        rows = None if self.allowed is None else torch.zeros(logits.shape[0], dtype=torch.int32, device=logits.device)
+        d = LogitsDesc(n_seqs=past.shape[0], total=logits.shape[0], vocab=logits.shape[1], dtype=_HAWQ[logits.dtype], past_stride=past.stride(0), n_bias=self.ids.numel(),
+                       n_allowed=0 if rows is None else 1, allowed_stride=0 if rows is None else self.allowed.stride(0), x_stride=logits.stride(0), y_stride=logits.stride(0))
+        hawq_logits(d, logits, past, past_lens, prompt_lens, starts, drafts, mask, self.penalties, self.starts, self.ids, self.values, self.allowed, rows, logits)
 
 
 def _norm(x):
@@ -56,7 +110,8 @@ def _norm(x):
 class Decoder:
     """The model, its cache, and the requests that hold pages of it."""
 
-    def __init__(self, n_requests, dtype=torch.bfloat16, cache="same", seed=0, config=CONFIG, most=1024):
+    def __init__(self, n_requests, dtype=torch.bfloat16, cache="same", seed=0, config=CONFIG, most=1024, whole=False, adapters=None, rules=None):
+        """whole: positions are rotary and the gate is the library's.  adapters: each request's own (0, 1 or 2; -1: none).  rules: Rules of the answers."""
         c = self.config = dict(config)
         self.dtype, self.n = dtype, n_requests
         r = np.random.default_rng(seed)
@@ -77,6 +132,14 @@ class Decoder:
         self.table = torch.full((n_requests, -(-most // c["page"])), -1, dtype=torch.int32, device="cuda")
         self.cached = torch.zeros(n_requests, dtype=torch.int32, device="cuda")
         self.lengths = [0] * n_requests                               # the same on the host
+        self.whole, self.rules = whole, rules
+        self.turns = torch.from_numpy(rotary_turns(D)).cuda()
+        self.adapters = None
+        if adapters is not None:
+            self.adapter = torch.tensor(adapters, dtype=torch.int32, device="cuda")
+            self.adapters = [Adapters(r, (4, 16, 8), (H + 2 * KV) * D, c["width"], dtype) for _ in range(c["layers"])]
+        self.past = torch.zeros((n_requests, self.table.shape[1] * c["page"]), dtype=torch.int32, device="cuda")      # the cached tokens themselves
+        self.prompt_lens = torch.zeros(n_requests, dtype=torch.int32, device="cuda")
 
     def _room(self, fresh):
         """Slots for `fresh[b]` more tokens of every request; their pages leave the free list."""
@@ -100,15 +163,31 @@ class Decoder:
         d = CacheStoreDesc(cache=self.cache_desc, total=k.shape[0], dtype=_HAWQ[self.dtype], **_strides(k=k, v=v))
         hawq_cache_store(d, k, v, slots, *self.caches[layer])
 
-    def _forward(self, tokens, attend):
-        """Logits of packed tokens; attend(layer, q, k, v, y) fills y."""
+    def _turn(self, q, k, positions):
+        """Queries and keys in place."""
+        c = self.config
+        d = RotaryDesc(total=q.shape[0], q_heads=c["q_heads"], kv_heads=c["kv_heads"], head_dim=c["head_dim"], rotary_dim=c["head_dim"], layout=ROTARY_HALVES, dtype=_HAWQ[self.dtype],
+                       scale=1.0, **_strides(q=q, k=k, yq=q, yk=k))
+        hawq_rotary(d, q, k, positions, self.turns, q, k)
+
+    def _forward(self, tokens, attend, positions, requests):
+        """Logits of packed tokens at their positions in their requests; attend(layer, q, k, v, y) fills y."""
         c, x = self.config, self.embedding[tokens]
         D, H, KV = c["head_dim"], c["q_heads"], c["kv_heads"]
         for i, layer in enumerate(self.layers):
-            qkv = layer["qkv"](_norm(x)).view(-1, H + 2 * KV, D)
+            inner = _norm(x)
+            qkv = layer["qkv"](inner)
+            if self.adapters is not None:
+                self.adapters[i].add(inner, qkv, self.adapter[requests])
+            qkv = qkv.view(-1, H + 2 * KV, D)
+            if self.whole:
+                self._turn(qkv[:, :H], qkv[:, H:H + KV], positions)
             y = torch.empty((qkv.shape[0], H, D), dtype=self.dtype, device="cuda")
             attend(i, qkv[:, :H], qkv[:, H:H + KV], qkv[:, H + KV:], y)
             x = x + layer["out"](y.view(-1, H * D))
+            if self.whole:
+                x = x + layer["down"](layer["up"].gated(_norm(x)))
+                continue
             gate, up = layer["up"](_norm(x)).chunk(2, dim=1)
             x = x + layer["down"]((torch.nn.functional.silu(gate.float()) * up.float()).to(self.dtype))
         return self.head(_norm(x))
@@ -123,9 +202,24 @@ class Decoder:
                                scale=c["head_dim"] ** -0.5, **_strides(q=q, k=k, v=v, y=y))
             hawq_attn_prompt(d, q, k, v, starts, y)
             self._store(i, k, v, slots)
-        logits = self._forward(torch.tensor([t for p in prompts for t in p], device="cuda"), attend)
+        positions = torch.tensor([t for n in lens for t in range(n)], dtype=torch.int32, device="cuda")
+        logits = self._forward(torch.tensor([t for p in prompts for t in p], device="cuda"), attend, positions, self._requests(lens))
+        for b, p in enumerate(prompts):
+            self.past[b, :len(p)] = torch.tensor(p, dtype=torch.int32)
+        self.prompt_lens.copy_(fresh)
         self._grow(lens, fresh)
         return logits
+
+    def _requests(self, lens):
+        return torch.tensor([b for b, n in enumerate(lens) for _ in range(n)], device="cuda")
+
+    def first(self, logits):
+        """Logits of the prompts' last tokens by the rules; logits: what `prompts` gave."""
+        ends = torch.cumsum(self.prompt_lens.long(), 0) - 1
+        rows = logits[ends]
+        if self.rules is not None:
+            self.rules.apply(rows, self.past, self.cached, self.prompt_lens)
+        return rows
 
     def check(self, drafts, masks):
         """Logits of drafted tokens (one list for each request, every token's mask over its own list); they are not stored yet."""
@@ -142,7 +236,15 @@ class Decoder:
                 self.workspace = torch.empty(hawq_attn_tree_workspace_bytes(d), dtype=torch.uint8, device="cuda")
             hawq_attn_tree(d, q, k, v, starts, mask, *self.caches[i], self.table, self.cached, y, self.workspace)
             self.drafted.append((k, v))
-        return self._forward(torch.tensor([t for d in drafts for t in d], device="cuda"), attend)
+        tokens = torch.tensor([t for d in drafts for t in d], device="cuda")
+        # a drafted token lies as many tokens behind the cache as it has ancestors
+        depth = torch.tensor([bin(m).count("1") - 1 for request in masks for m in request], dtype=torch.int32, device="cuda")
+        requests = self._requests(lens)
+        logits = self._forward(tokens, attend, self.cached[requests] + depth, requests)
+        self.tokens = tokens.to(torch.int32)
+        if self.rules is not None:
+            self.rules.apply(logits, self.past, self.cached, self.prompt_lens, starts, self.tokens, mask)
+        return logits
 
     def keep(self, lens, kept):
         """Stores what was kept of the last check's drafts: kept[b] are rows of request b, in order."""
@@ -153,6 +255,8 @@ class Decoder:
         at[torch.tensor(rows, device="cuda")] = slots
         for i, (k, v) in enumerate(self.drafted):
             self._store(i, k, v, at)
+        for b, k in enumerate(kept):
+            self.past[b, self.lengths[b]:self.lengths[b] + len(k)] = self.tokens[[int(first[b]) + i for i in k]]
         self._grow([len(k) for k in kept], fresh)
 
 
@@ -173,8 +277,7 @@ def _draft(last, memory, width=2, depth=3):
 
 def generate(model, prompts, n_tokens, drafting=True):
     """Greedy answers of n_tokens each, the number of passes that they took, and the tokens written in all (requests that drafted well are ahead)."""
-    ends = np.cumsum([len(p) for p in prompts]) - 1
-    out = [[int(t)] for t in model.prompts(prompts)[torch.from_numpy(ends).cuda()].argmax(dim=1)]
+    out = [[int(t)] for t in model.first(model.prompts(prompts)).argmax(dim=1)]
     memory, passes = [{} for _ in prompts], 0
     for m, p in zip(memory, prompts):
         for a, b in zip(p, p[1:]):
@@ -204,10 +307,12 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--cache", choices=("same", "s8"), default="same")
     ap.add_argument("--tokens", type=int, default=24)
+    ap.add_argument("--whole", action="store_true", help="rotary positions, the fused gate, adapters and rules for the answers")
     a = ap.parse_args()
     r = np.random.default_rng(1)
     prompts = [r.integers(0, CONFIG["vocab"], size=n).tolist() for n in (5, 37, 1, 18)]
-    answers, passes, written = generate(Decoder(len(prompts), cache=a.cache), prompts, a.tokens)
+    more = dict(whole=True, adapters=[0, 2, -1, 1], rules=Rules(len(prompts), CONFIG["vocab"], (1.3, 0.5, 0.2), {7: -100.0}, range(0, CONFIG["vocab"], 2))) if a.whole else {}
+    answers, passes, written = generate(Decoder(len(prompts), cache=a.cache, **more), prompts, a.tokens)
     for p, o in zip(prompts, answers):
         print("%d tokens -> %s" % (len(p), o))
     print("%d passes after the prompts, %.2f tokens of a request in a pass" % (passes, (written / len(prompts) - 1) / passes))
