@@ -1,13 +1,17 @@
 // What a server does to the logits before it chooses: penalties for tokens that occurred, biases, grammar masks.
 //
-// A workgroup takes a part of the vocabulary for one row.  It copies the part with the mask applied, eight logits to a thread, in place only
-// what the mask takes away; that waits for nothing but the mask.  Meanwhile it counts the past tokens of the row's request that fall into the
-// part in LDS, one word a token (bit 31: occurred; bits 24 to 30: its place in a short list of biases; below: how often the model wrote it), and
-// the drafted tokens that the row sees.  Whoever counted a token then takes its word away: the first one writes the token's logit again.  With a
-// long list the part is counted in two halves, the second half of LDS holding the places.  Integer counts and maxima: the order of the atomics
-// does not matter.
+// Two things are done to a row.  Its logits are copied with the mask applied, eight to a thread (in place: only what the mask takes away).  And
+// the tokens that occurred or are listed are counted in LDS, one word a token (bit 31: occurred; bits 24 to 30: its place in a short list of
+// biases; below: how often the model wrote it), whose logits are then written again.  Integer counts and maxima: the order of the atomics does not
+// matter.
 //
-// Bound by the logits' bytes for many rows, by a chain of loads (request, lengths, tokens) and a launch for few.
+// Few logits go through one launch: a workgroup copies a part of the vocabulary and counts the tokens that fall into it, words lying by token.
+// Many go through two: a copy that waits for nothing but the mask, and a workgroup for each row, whose words lie by a hash of the token,
+// so that the row's tokens are read once.  Rows with more tokens or longer lists than that holds go part by part there, too.
+//
+// Bound by the logits' bytes for many rows, by a chain of loads (request, lengths, tokens, logits) and a launch for few.  Measured: 256 x 128001
+// 43 us, of which the copy alone is 27 (4.9 TB/s) and the tokens 13; 171 x 64000 18; one row of 32000 6, twice an empty launch.  Words checked in
+// order instead of by token, in one launch: 256 x 128001 64 us and more, the copy's loop no longer in the instruction cache.
 #include "lm.h"
 #include "lm_launch.h"
 
@@ -15,11 +19,14 @@ namespace hawq {
 
 namespace {
 
-constexpr uint32_t kOccurred = 0x80000000u, kPlace = 0x7F000000u, kCount = 0x00FFFFFFu;
-constexpr int kThreads = 512, kAhead = 4;        // eights of a thread on their way while the tokens are counted
-constexpr int kFewBiases = 127, kTokens = 4;     // tokens of a thread under way
+constexpr uint32_t kOccurred = 0x80000000u, kPlaces = 0x7F000000u, kListed = 1u << 24, kCount = 0x00FFFFFFu;
+constexpr int kFewBiases = 127;                  // whose places a word holds
+constexpr int kPartThreads = 512, kAhead = 4;    // eights of a thread on their way while the request is looked for
+// Logits from which tokens are counted in a launch of their own: 171 x 64000 take 18.5 us in one launch and 20.9 in two, 256 x 128001 61 and 43.
+constexpr int64_t kApart = 1 << 24;
+constexpr int kRowThreads = 1024, kSlots = 16384, kMostHashed = 10000;
 
-// The request whose rows t belongs to, -1: none.  64 places at a time: the lengths' chain of loads is one or two long.
+// The request whose rows t belongs to, -1: none.  64 places at a time: the chain of loads is one or two long, up to 2^24 requests four.
 __device__ __forceinline__ int request_of(const LogitsArgs &a, int t) {
     if (!a.starts) return t;
     const int lane = threadIdx.x & 63;
@@ -43,19 +50,148 @@ __device__ __forceinline__ int request_of(const LogitsArgs &a, int t) {
     return known && a.starts[low] <= t ? low : -1;
 }
 
-// the larger of a word's place (bits 24 to 30) and this one, beside whatever else changes the word
+// the larger of a word's place and this one, beside whatever else changes the word
 __device__ __forceinline__ void highest(uint32_t *word, uint32_t place) {
     uint32_t had = *(volatile uint32_t *)word;
     while ((had >> 24 & 127u) < place) {
-        const uint32_t now = atomicCAS(word, had, (had & ~kPlace) | place << 24);
+        const uint32_t now = atomicCAS(word, had, (had & ~kPlaces) | place << 24);
         if (now == had) return;
         had = now;
     }
 }
 
-// IN_PLACE: y is x, and what does not change is neither read nor written.
-template <class T, bool IN_PLACE>
-__global__ __launch_bounds__(kThreads) void logits_part(LogitsArgs a, int part) {
+template <class T, int THREADS>
+struct Row {
+    typedef typename T::elem E;
+    const E *x;
+    E *y;
+    float r, presence, frequency;
+    const int32_t *bias_ids, *past, *drafts;
+    const float *bias_values;
+    const uint32_t *allowed;                     // nullptr: everything
+    uint64_t sees;                               // of 64 drafts; all ones without a mask
+    int biases, len, prompt, seen;               // numbers of listed, past and drafted tokens
+    bool counts;
+    int32_t listed, draft, head[4];              // this thread's first listed, drafted and past tokens
+
+    // what is known of row t of request b, all at once: every load that waits for another costs a microsecond
+    __device__ __forceinline__ void load(const LogitsArgs &a, int t, int b) {
+        x = (const E *)a.x + t * a.x_stride;
+        y = (E *)a.y + t * a.y_stride;
+        const int64_t p = 3 * (int64_t)b;
+        r = a.penalties ? a.penalties[p] : 1.f;
+        presence = a.penalties ? a.penalties[p + 1] : 0.f;
+        frequency = a.penalties ? a.penalties[p + 2] : 0.f;
+        const int first = a.n_bias > 0 ? min(max(a.bias_starts[b], 0), a.n_bias) : 0;
+        biases = a.n_bias > 0 ? min(max(a.bias_starts[b + 1], first), a.n_bias) - first : 0;
+        bias_ids = a.bias_ids + first;
+        bias_values = a.bias_values + first;
+        len = a.past_stride > 0 ? min(max(a.past_lens[b], 0), a.past_stride) : 0;
+        prompt = a.past_stride > 0 && a.prompt_lens ? a.prompt_lens[b] : 0;
+        past = a.past + (int64_t)b * a.past_stride;
+        int from = t, to = t + 1;
+        if (a.drafts && a.starts) sequence_rows(a.starts, b, a.total, from, to);
+        drafts = a.drafts ? a.drafts + from : nullptr;
+        sees = a.drafts && a.mask ? a.mask[t] : ~0ull;
+        seen = !a.drafts ? 0 : a.mask ? min(to - from, 64) : t + 1 - from;
+        const int row = a.n_allowed == 0 ? -1 : a.allowed_row ? a.allowed_row[t] : t;
+        allowed = row >= 0 && row < a.n_allowed ? a.allowed + row * a.allowed_stride : nullptr;
+        counts = r != 1.f || presence != 0.f || frequency != 0.f;
+        if (!counts) len = seen = 0;
+        listed = biases > 0 ? bias_ids[min((int)threadIdx.x, biases - 1)] : -1;
+        draft = seen > 0 ? drafts[min((int)threadIdx.x, seen - 1)] : -1;
+        for (int i = 0; i < 4; ++i) head[i] = len > 0 ? past[min((int)threadIdx.x + i * THREADS, len - 1)] : -1;
+    }
+
+    // f(token, entry of the list or -1, whether the model wrote it) of this thread's share of all
+    template <class F>
+    __device__ __forceinline__ void each(F &&f) const {
+        for (int i = threadIdx.x; i < biases; i += THREADS) f(i < THREADS ? listed : bias_ids[i], i, false);
+        for (int i = threadIdx.x; i < seen; i += THREADS) f(sees >> (i & 63) & 1 ? i < THREADS ? draft : drafts[i] : -1, -1, true);      // (-1 is no token)
+        // (four on their way at a time)
+        for (int i0 = threadIdx.x; i0 < len; i0 += 4 * THREADS) {
+            int32_t token[4];
+            for (int i = 0; i < 4; ++i) token[i] = i0 < THREADS ? head[i] : past[min(i0 + i * THREADS, len - 1)];
+            for (int i = 0; i < 4; ++i)
+                if (i0 + i * THREADS < len) f(token[i], -1, i0 + i * THREADS >= prompt);
+        }
+    }
+
+    // the logits of tokens v[i] with words c[i], 0: none; place: entries of the list and 1, 0: not in it
+    template <int N>
+    __device__ __forceinline__ void again(const int (&v)[N], const uint32_t (&c)[N], const uint32_t (&place)[N]) const {
+        E l[N];
+        float bias[N];
+        uint32_t kept[N];
+        for (int i = 0; i < N; ++i) {
+            const int at = c[i] ? v[i] : 0;
+            l[i] = x[at];
+            kept[i] = c[i] ? allowed ? allowed[at >> 5] >> (at & 31) & 1 : 1 : 0;
+            bias[i] = place[i] ? bias_values[place[i] - 1] : 0.f;
+        }
+        for (int i = 0; i < N; ++i) {
+            float n = (float)l[i];
+            if (c[i] & kOccurred) n = n > 0 ? n / r : n * r;
+            if (c[i] & kCount) n = n - frequency * (float)(c[i] & kCount) - presence;
+            if (place[i]) n += bias[i];
+            if (kept[i]) y[v[i]] = (E)n;
+        }
+    }
+
+    // The tokens v0 .. v0 + n - 1 by words of their own, count[n], and where the list is long place[n]; both with three words to spare.
+    // Whoever counted a token takes its word away afterwards: the first one writes the token's logit again.
+    __device__ __forceinline__ void settle(int v0, int n, uint32_t *count, uint32_t *place) const {
+        const bool places = biases > kFewBiases;
+        for (int i = threadIdx.x; i < (n + 3) / 4; i += THREADS) {
+            ((v4u *)count)[i] = v4u{0, 0, 0, 0};
+            if (places) ((v4u *)place)[i] = v4u{0, 0, 0, 0};
+        }
+        __syncthreads();
+        each([&](int32_t token, int entry, bool written) {
+            const uint32_t at = (uint32_t)token - (uint32_t)v0;
+            if (at >= (uint32_t)n) return;
+            if (entry >= 0) {
+                if (places) atomicMax(place + at, (uint32_t)entry + 1), atomicOr(count + at, kListed);
+                else highest(count + at, (uint32_t)entry + 1);
+            } else {
+                if (written) atomicAdd(count + at, 1u);
+                atomicOr(count + at, kOccurred);
+            }
+        });
+        __syncthreads();
+        auto take = [&](auto &token) {
+            constexpr int N = sizeof(token) / sizeof(token[0]);
+            bool any = false;
+            for (int i = 0; i < N; ++i) any |= (uint32_t)token[i] - (uint32_t)v0 < (uint32_t)n;
+            if (!any) return;
+            uint32_t c[N], l[N];
+            for (int i = 0; i < N; ++i) {
+                const uint32_t at = (uint32_t)token[i] - (uint32_t)v0;
+                c[i] = at < (uint32_t)n ? atomicExch(count + at, 0u) : 0u;
+            }
+            for (int i = 0; i < N; ++i) l[i] = !(c[i] & kPlaces) ? 0u : places ? place[(uint32_t)token[i] - (uint32_t)v0] : c[i] >> 24 & 127u;
+            again(token, c, l);
+        };
+        for (int i = threadIdx.x; i < biases; i += THREADS) {
+            const int32_t token[1] = {i < THREADS ? listed : bias_ids[i]};
+            take(token);
+        }
+        for (int i = threadIdx.x; i < seen; i += THREADS) {
+            const int32_t token[1] = {i < THREADS ? draft : drafts[i]};
+            take(token);
+        }
+        for (int i0 = threadIdx.x; i0 < len; i0 += 4 * THREADS) {
+            int32_t token[4];                    // (past the last one: that one again)
+            for (int i = 0; i < 4; ++i) token[i] = i0 < THREADS ? head[i] : past[min(i0 + i * THREADS, len - 1)];
+            take(token);
+        }
+        __syncthreads();
+    }
+};
+
+// IN_PLACE: y is x, and what does not change is neither read nor written.  WORDS: tokens are counted here, too.
+template <class T, bool IN_PLACE, bool WORDS>
+__global__ __launch_bounds__(kPartThreads) void logits_part(LogitsArgs a, int part) {
     typedef typename T::elem E;
     typedef uint32_t Eight __attribute__((ext_vector_type(4), aligned(2)));      // (rows of x lie at any element)
     extern __shared__ __align__(16) uint32_t words[];
@@ -70,44 +206,20 @@ __global__ __launch_bounds__(kThreads) void logits_part(LogitsArgs a, int part) 
     Eight ahead[kAhead];
     if (!IN_PLACE)
         for (int i = 0; i < kAhead; ++i) {
-            const int k = threadIdx.x + i * kThreads;
+            const int k = threadIdx.x + i * kPartThreads;
             if (k < eights && whole(k)) ahead[i] = *(const Eight *)(x + (8 * k - off));
         }
     const int b = request_of(a, t);
     if (b < 0) return;
-    // what is known of the request, all at once: every load that waits for another costs a microsecond
-    const int64_t pen = 3 * (int64_t)b;
-    const float r = a.penalties ? a.penalties[pen] : 1.f, presence = a.penalties ? a.penalties[pen + 1] : 0.f, frequency = a.penalties ? a.penalties[pen + 2] : 0.f;
-    const int first_bias = a.n_bias > 0 ? min(max(a.bias_starts[b], 0), a.n_bias) : 0, last_bias = a.n_bias > 0 ? min(max(a.bias_starts[b + 1], first_bias), a.n_bias) : 0;
-    const int len = a.past_stride > 0 ? min(max(a.past_lens[b], 0), a.past_stride) : 0, prompt = a.past_stride > 0 && a.prompt_lens ? a.prompt_lens[b] : 0;
-    const int mask_row = a.n_allowed == 0 ? -1 : a.allowed_row ? a.allowed_row[t] : t;
-    int from = t, to = t + 1;
-    if (a.drafts && a.starts) sequence_rows(a.starts, b, a.total, from, to);
-    const uint64_t sees = a.drafts && a.mask ? a.mask[t] : ~0ull;
-    const int seen = !a.drafts ? 0 : a.mask ? min(to - from, 64) : t + 1 - from;
-    const bool counts = r != 1.f || presence != 0.f || frequency != 0.f, biases = last_bias > first_bias;
-    const uint32_t *const allowed = mask_row >= 0 && mask_row < a.n_allowed ? a.allowed + mask_row * a.allowed_stride : nullptr;
-    const int32_t *const past = a.past + (int64_t)b * a.past_stride;
-    const int32_t listed = biases ? a.bias_ids[min(first_bias + (int)threadIdx.x, last_bias - 1)] : -1, draft = seen > 0 ? a.drafts[from + min((int)threadIdx.x, seen - 1)] : -1;
-    // this thread's tokens from i0 on, -1 past the last; the first ones
-    struct Tokens { int32_t id[kTokens]; };
-    auto read = [&](int i0) {
-        Tokens k;
-        for (int i = 0; i < kTokens; ++i) {
-            const int p = i0 + i * kThreads + (int)threadIdx.x;
-            k.id[i] = past[min(p, len - 1)];
-            if (p >= len) k.id[i] = -1;
-        }
-        return k;
-    };
-    Tokens head;
-    if (counts && len > 0) head = read(0);
-    auto may = [&](int v) { return !allowed || (allowed[v >> 5] >> (v & 31) & 1); };
+    Row<T, kPartThreads> row;
+    row.load(a, t, b);
+    const uint32_t *const allowed = row.allowed;
     auto copy = [&](int k, Eight d) {
         const int at = 8 * k - off;              // of the eight's first element in the part
         if (!whole(k)) {
+#pragma unroll 1
             for (int i = max(at, 0); i < min(at + 8, n); ++i) {
-                const bool kept = may(v0 + i);
+                const bool kept = !allowed || (allowed[(v0 + i) >> 5] >> ((v0 + i) & 31) & 1);
                 if (!IN_PLACE || !kept) y[i] = kept ? x[i] : (E)-INFINITY;
             }
             return;
@@ -129,114 +241,99 @@ __global__ __launch_bounds__(kThreads) void logits_part(LogitsArgs a, int part) 
                 if (!(bits >> i & 1)) e[i] = (E)-INFINITY;
         *(v4u *)(y + at) = __builtin_bit_cast(v4u, e);
     };
-    if (!IN_PLACE || allowed)
+    if (!IN_PLACE || allowed) {
         for (int i = 0; i < kAhead; ++i) {
-            const int k = threadIdx.x + i * kThreads;
+            const int k = threadIdx.x + i * kPartThreads;
             if (k < eights) copy(k, ahead[i]);
         }
-    if (!IN_PLACE || allowed)
-        for (int k = threadIdx.x + kAhead * kThreads; k < eights; k += kThreads) {
+        for (int k = threadIdx.x + kAhead * kPartThreads; k < eights; k += kPartThreads) {
             Eight d{0, 0, 0, 0};
             if (!IN_PLACE && whole(k)) d = *(const Eight *)(x + (8 * k - off));
             copy(k, d);
         }
-    if (!counts && !biases) return;
-
-    const bool places = last_bias - first_bias > kFewBiases;
-    const int per = places ? (part + 1) >> 1 : part;
-    uint32_t *const count = words, *const place = words + per;              // place: i + 1 for entry i of the list
-    for (int first = 0; first < n; first += per) {
-        const int some = min(per, n - first);                               // tokens v0 + first and on
-        for (int i = threadIdx.x; i < (part + 4) / 4; i += kThreads) ((v4u *)words)[i] = v4u{0, 0, 0, 0};
-        __syncthreads();
-        auto place_of = [&](int32_t token) { return (uint32_t)token - (uint32_t)(v0 + first); };      // below `some` if it is one of these
-        // bit i: token i is one of these
-        auto hits_of = [&](const Tokens &k) {
-            uint32_t hits = 0;
-            for (int i = 0; i < kTokens; ++i) hits |= place_of(k.id[i]) < (uint32_t)some ? 1u << i : 0u;
-            return hits;
-        };
-        auto tally = [&](const Tokens &k, int i0) {
-            const uint32_t hits = hits_of(k);
-            if (hits)
-                for (int i = 0; i < kTokens; ++i)
-                    if (hits >> i & 1) {
-                        uint32_t *const word = count + place_of(k.id[i]);
-                        if (i0 + i * kThreads + (int)threadIdx.x >= prompt) atomicAdd(word, 1u);
-                        atomicOr(word, kOccurred);
-                    }
-        };
-        // the logit of a token whose word c was taken away
-        auto again = [&](uint32_t at, uint32_t c) {
-            const int e = first + (int)at;
-            const E l = x[e];
-            const float bias = c & kPlace ? a.bias_values[first_bias + (int)(places ? place[at] : c >> 24 & 127u) - 1] : 0.f;
-            if (!may(v0 + e)) return;
-            float v = (float)l;
-            if (c & kOccurred) v = v > 0 ? v / r : v * r;
-            if (c & kCount) v = v - frequency * (float)(c & kCount) - presence;
-            if (c & kPlace) v += bias;
-            y[e] = (E)v;
-        };
-        auto settle = [&](const Tokens &k) {
-            const uint32_t hits = hits_of(k);
-            if (hits) {
-                uint32_t c[kTokens];
-                for (int i = 0; i < kTokens; ++i) c[i] = hits >> i & 1 ? atomicExch(count + place_of(k.id[i]), 0u) : 0u;
-                for (int i = 0; i < kTokens; ++i)
-                    if (c[i]) again(place_of(k.id[i]), c[i]);
-            }
-        };
-        auto settle_one = [&](int32_t token) {
-            const uint32_t at = place_of(token), c = at < (uint32_t)some ? atomicExch(count + at, 0u) : 0u;
-            if (c) again(at, c);
-        };
-        for (int i = threadIdx.x; i < last_bias - first_bias; i += kThreads) {
-            const uint32_t at = place_of(i < kThreads ? listed : a.bias_ids[first_bias + i]);
-            if (at >= (uint32_t)some) continue;
-            if (places) atomicMax(place + at, (uint32_t)i + 1), atomicOr(count + at, 1u << 24);
-            else highest(count + at, (uint32_t)i + 1);
-        }
-        if (counts) {
-            for (int i = threadIdx.x; i < seen; i += kThreads) {
-                const uint32_t at = place_of(i < kThreads ? draft : a.drafts[from + i]);
-                if (at < (uint32_t)some && (!a.mask || (sees >> i & 1))) {
-                    atomicAdd(count + at, 1u);
-                    atomicOr(count + at, kOccurred);
-                }
-            }
-            if (len > 0) tally(head, 0);
-            for (int i0 = kTokens * kThreads; i0 < len; i0 += kTokens * kThreads) tally(read(i0), i0);
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < last_bias - first_bias; i += kThreads) settle_one(i < kThreads ? listed : a.bias_ids[first_bias + i]);
-        if (counts) {
-            for (int i = threadIdx.x; i < seen; i += kThreads) settle_one(i < kThreads ? draft : a.drafts[from + i]);
-            if (len > 0) settle(head);
-            for (int i0 = kTokens * kThreads; i0 < len; i0 += kTokens * kThreads) settle(read(i0));
-        }
-        if (first + per < n) __syncthreads();
     }
+    if (!WORDS || (!row.counts && row.biases == 0)) return;
+    __syncthreads();                             // (what is written again comes after what was copied)
+    const int half = row.biases > kFewBiases ? (part / 2 + 3) & ~3 : part;       // a long list's places share the words
+    for (int first = 0; first < n; first += half) row.settle(v0 + first, min(half, n - first), words, words + half);
+}
+
+// The tokens of one row, behind its copy.
+template <class T>
+__global__ __launch_bounds__(kRowThreads) void logits_row(LogitsArgs a) {
+    extern __shared__ __align__(16) uint32_t words[];
+    const int t = (int)((int64_t)blockIdx.y * gridDim.x + blockIdx.x);
+    if (t >= a.total) return;
+    const int b = request_of(a, t);
+    if (b < 0) return;
+    Row<T, kRowThreads> row;
+    row.load(a, t, b);
+    const int64_t tokens = (int64_t)row.len + row.seen + row.biases;
+    if (tokens == 0) return;
+    if (tokens > kMostHashed || row.biases > kFewBiases) {
+        for (int64_t v = 0; v < a.vocab; v += kSlots) row.settle((int)v, (int)min((int64_t)kSlots, a.vocab - v), words, words + kSlots);
+        return;
+    }
+    // slots of a token and a word, half as many again as tokens or more: 4096, 8192 or 16384
+    uint32_t *const key = words, *const count = words + kSlots;
+    const int bits = tokens <= 2700 ? 12 : tokens <= 5400 ? 13 : 14, slots = 1 << bits;
+    for (int i = threadIdx.x; i < slots / 4; i += kRowThreads) {
+        ((v4u *)key)[i] = v4u{0, 0, 0, 0};
+        ((v4u *)count)[i] = v4u{0, 0, 0, 0};
+    }
+    __syncthreads();
+    row.each([&](int32_t token, int entry, bool written) {
+        if ((uint32_t)token >= (uint32_t)a.vocab) return;
+        uint32_t at = (uint32_t)token * 2654435761u >> (32 - bits);
+        for (;;) {                               // (ends: there are more slots than tokens)
+            const uint32_t had = atomicCAS(key + at, 0u, (uint32_t)token + 1);
+            if (had == 0 || had == (uint32_t)token + 1) break;
+            at = (at + 1) & (slots - 1);
+        }
+        if (entry >= 0) {
+            highest(count + at, (uint32_t)entry + 1);
+        } else {
+            if (written) atomicAdd(count + at, 1u);
+            atomicOr(count + at, kOccurred);
+        }
+    });
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < slots / 4; i += kRowThreads) {
+        const v4u k = ((const v4u *)key)[i], c = ((const v4u *)count)[i];
+        const int v[4] = {(int)k.x - 1, (int)k.y - 1, (int)k.z - 1, (int)k.w - 1};      // (an empty slot's word is 0)
+        const uint32_t words_of[4] = {c.x, c.y, c.z, c.w}, places[4] = {c.x >> 24 & 127u, c.y >> 24 & 127u, c.z >> 24 & 127u, c.w >> 24 & 127u};
+        if (c.x | c.y | c.z | c.w) row.again(v, words_of, places);
+    }
+}
+
+template <class T, bool IN_PLACE>
+hawq_status launch(const LogitsArgs &a, hipStream_t s) {
+    const bool counted = a.penalties || a.n_bias > 0, copied = !IN_PLACE || a.n_allowed > 0;
+    const bool apart = counted && (!copied || (int64_t)a.total * a.vocab >= kApart);
+    if (copied) {
+        // parts of 16384 tokens, smaller ones where that gives the 256 compute units less than four each
+        int part = 16384;
+        while (part > 1024 && (int64_t)a.total * ((a.vocab + part - 1) / part) < 1024) part /= 2;
+        const int64_t along = a.total < kMostAlong ? a.total : kMostAlong;
+        const dim3 grid((unsigned)(((int64_t)a.vocab + part - 1) / part), (unsigned)along, (unsigned)((a.total + along - 1) / along));
+        if (counted && !apart) logits_part<T, IN_PLACE, true><<<grid, kPartThreads, (size_t)(part + 16) * 4, s>>>(a, part);
+        else logits_part<T, IN_PLACE, false><<<grid, kPartThreads, 0, s>>>(a, part);
+        const hawq_status st = check_launch();
+        if (st != HAWQ_OK) return st;
+    }
+    if (!apart) return HAWQ_OK;
+    const Grid g = spread(a.total, 1, kRowThreads);
+    if (g.x == 0) return HAWQ_ERR_UNSUPPORTED;
+    logits_row<T><<<dim3((unsigned)g.x, (unsigned)g.y), kRowThreads, 2 * kSlots * 4, s>>>(a);
+    return check_launch();
 }
 
 }  // namespace
 
 hawq_status launch_logits(const LogitsArgs &a, hipStream_t s) {
-    // parts of 16384 tokens, smaller ones where that gives the 256 compute units less than four each
-    int part = 16384;
-    while (part > 1024 && (int64_t)a.total * ((a.vocab + part - 1) / part) < 1024) part /= 2;
-    const int64_t along = a.total < kMostAlong ? a.total : kMostAlong;
-    const dim3 grid((unsigned)(((int64_t)a.vocab + part - 1) / part), (unsigned)along, (unsigned)((a.total + along - 1) / along));
-    const size_t lds = (size_t)(part + 32) * 4;
-    const bool in_place = a.x == a.y;
-    if (a.dtype == HAWQ_F16) {
-        if (in_place) logits_part<F16, true><<<grid, kThreads, lds, s>>>(a, part);
-        else logits_part<F16, false><<<grid, kThreads, lds, s>>>(a, part);
-    } else {
-        if (in_place) logits_part<BF16, true><<<grid, kThreads, lds, s>>>(a, part);
-        else logits_part<BF16, false><<<grid, kThreads, lds, s>>>(a, part);
-    }
-    return check_launch();
+    if (a.dtype == HAWQ_F16) return a.x == a.y ? launch<F16, true>(a, s) : launch<F16, false>(a, s);
+    return a.x == a.y ? launch<BF16, true>(a, s) : launch<BF16, false>(a, s);
 }
 
 }  // namespace hawq

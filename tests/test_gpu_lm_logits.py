@@ -187,3 +187,17 @@ def test_one_row_of_logits_for_all():
     for b in range(3):
         want[b, 2 * b:2 * b + 2] -= 1.5
     assert torch.equal(y, want.half())
+
+
+@pytest.mark.parametrize("past", [2000, 2699, 2700, 5400, 5401, 9990, 10001, 15000])
+@pytest.mark.parametrize("few", [None, 50])
+def test_what_changes_in_place(past, few):
+    """In place without masks only the tokens that occurred or are listed are touched, however many there are."""
+    _run([1, 2], 20001, [past, past // 2], "bf16", biases=8, in_place=True, few=few, seed=past)
+    _run([1, 2], 20001, [past, 10], "f16", biases=400, in_place=True, few=few, seed=past)
+
+
+def test_many_logits():
+    """Past 2^24 logits, with drafts, masks, short and long lists, and rows behind the last request."""
+    _run([5] * 25 + [4], 131073, [40 * i for i in range(26)], "bf16", biases=60, masks=20, pad=3, behind=1, seed=1)
+    _run([1] * 33, 600001, [1000] * 32 + [11000], "f16", biases=300, masks=5, in_place=True, few=3000, seed=2)
