@@ -19,7 +19,8 @@ namespace hawq {
 namespace {
 
 constexpr int kRows = 128, kOuts = 128, kStep = 64, kThreads = 512;
-constexpr int kMostInputs = 1 << 16, kMostXStride = 1 << 22;       // of the prompt kernel: 32-bit offsets, a row's sums in LDS
+// Of the prompt kernel: a row's sums in LDS, 32-bit offsets, a launch of all tiles of rows.
+constexpr int kMostInputs = 1 << 16, kMostXStride = 1 << 22, kMostTall = 1 << 29;
 
 // v as three bf16 parts, each the one below its rest's (towards zero), and the operand {1, 1, 2, 2, 3, 0, 0, 0} of them
 __device__ __forceinline__ v4u three_parts(float v) {
@@ -363,7 +364,7 @@ hawq_status few_rows(const LinearW4Args &a, hipStream_t s) {
 
 // What the prompt kernel takes by its sizes (the workspace goes by them alone), and by its addresses.
 bool prompt_sized(const LinearW4Args &a) {
-    if (a.M <= 16 || a.K > kMostInputs || a.x_stride > kMostXStride || a.K % 32 != 0 || a.x_stride % 8 != 0) return false;
+    if (a.M <= 16 || a.M > kMostTall || a.K > kMostInputs || a.x_stride > kMostXStride || a.K % 32 != 0 || a.x_stride % 8 != 0) return false;
     const float more = a.group % 128 == 0 ? 1.f : a.group % 64 == 0 ? kScaledTwice : kScaledFour;
     return more * time_of(kPrompt, a) < time_of(kForms[best_form(a, 0x1f)], a);
 }

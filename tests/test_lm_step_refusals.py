@@ -68,6 +68,8 @@ def test_gated(lib):
     assert hawq.hawq_gated_w4_workspace_bytes(hawq.GatedW4Desc(**dict(base, M=-1))) == 0
     wide = dict(base, M=4000, N=4096, K=4096, x_stride=4096, y_stride=4096)
     need = hawq.hawq_gated_w4_workspace_bytes(hawq.GatedW4Desc(**wide))
+    for M in ((1 << 29) + 1, (1 << 31) - 4096):         # more rows than a launch of the prompts' form has workgroups for
+        assert hawq.hawq_gated_w4_workspace_bytes(hawq.GatedW4Desc(**dict(wide, M=M, x_stride=0))) == 0
     if need:
         assert call(bytes=need - 1, **wide) == WORKSPACE and call(workspace=None, **wide) == NULL and call(workspace=ctypes.c_void_p(4104), **wide) == UNSUPPORTED
 
