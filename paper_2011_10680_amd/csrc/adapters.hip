@@ -112,22 +112,23 @@ __device__ __forceinline__ void inner_tile(const AdaptersArgs &a, int m0, int id
         }
     }
     constexpr int kRow = 16 * NT + 4;
-    for (int i = 0; i < MT; ++i) {
-        __syncthreads();
-        for (int t = 0; t < NT; ++t) *(v4f *)(red + (wave * 16 + r) * kRow + 16 * t + 4 * c) = acc[i][t];
-        __syncthreads();
-        for (int e = threadIdx.x; e < 256 * NT; e += 64 * waves_of(MT)) {
-            const int m = e / (16 * NT), j = e % (16 * NT);
-            float v = 0;
-            for (int w = 0; w < waves_of(MT); ++w) v += red[(w * 16 + m) * kRow + j];
-            if ((rows >> (16 * i + m) & 1) && rb + j < rank) h[(int64_t)(m0 + 16 * i + m) * a.max_rank + rb + j] = v;
-        }
+    __syncthreads();
+    for (int i = 0; i < MT; ++i)
+        for (int t = 0; t < NT; ++t) *(v4f *)(red + ((wave * MT + i) * 16 + r) * kRow + 16 * t + 4 * c) = acc[i][t];
+    __syncthreads();
+    for (int e = threadIdx.x; e < 64 * NT * MT; e += 64 * waves_of(MT)) {
+        const int m = e / (4 * NT), j = e % (4 * NT) * 4;
+        v4f v{0, 0, 0, 0};
+        for (int w = 0; w < waves_of(MT); ++w) v += *(const v4f *)(red + (w * MT * 16 + m) * kRow + j);
+        if (rows >> m & 1)
+            for (int f = 0; f < 4; ++f)
+                if (rb + j + f < rank) h[(int64_t)(m0 + m) * a.max_rank + rb + j + f] = v[f];
     }
 }
 
 template <class T, int MT, bool VECTOR>
 __global__ __launch_bounds__(64 * waves_of(MT)) void inner(AdaptersArgs a, int slots, int splits) {
-    __shared__ __align__(16) float red[waves_of(MT) * 16 * 68];
+    __shared__ __align__(16) float red[waves_of(MT) * MT * 16 * 68];
     const int64_t tile = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (tile * (16 * MT) >= a.M) return;
     const int m0 = (int)tile * (16 * MT), slot = blockIdx.z % slots, split = blockIdx.z / slots;
