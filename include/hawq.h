@@ -554,7 +554,8 @@ hawq_status hawq_rotary(const hawq_rotary_desc *desc, const void *q, const void 
  * The first half of a gated feed-forward block from 4-bit weights: both projections, the activation and their product,
  *   y[m,n] = act(g) * u,   g = sum_k x[m,k] * W[n,k] (+ bias[n]),   u = sum_k x[m,k] * W[N + n,k] (+ bias[N + n])
  * W [2 N, K] as in hawq_linear_w4 (codes, zero points, scales and bias of 2 N rows, the gate's first), with the same types, strides,
- * sizes and accuracy of g and u, which stay in 32 bits; the result is rounded once.  Infinities and NaN give what the formula gives.
+ * sizes (N up to 2^30) and accuracy of g and u, which stay in 32 bits; the result is rounded once.  Infinities and NaN give what the
+ * formula gives.
  * act:  HAWQ_SILU g / (1 + exp(-g));  HAWQ_GELU g Phi(g), Phi the normal distribution's;  HAWQ_GELU_TANH its approximation
  * g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3)));  HAWQ_RELU max(g, 0).
  * workspace: device memory of hawq_gated_w4_workspace_bytes(desc) bytes (0 for few rows or an invalid desc), 16-byte aligned, scratch.
@@ -577,10 +578,11 @@ hawq_status hawq_gated_w4(const hawq_gated_w4_desc *desc, const void *x, const v
  *   y[m,n] = base[m,n] + scales[i] * sum_j b[i,n,j] * sum_k a[i,j,k] * x[m,k],   i = adapter[m],   j < ranks[i]
  * x [M, K], base and y [M, N], a [n_adapters, max_rank, K], b [n_adapters, N, max_rank] of T with the strides given (elements of a_row and
  * b_row are contiguous; strides of what is read may be 0); adapter int32 [M], ranks int32 [n_adapters] (as 0..max_rank), scales
- * float32 [n_adapters].  A row whose adapter is not one of 0..n_adapters - 1 (as -1) gets base as it is.  What lies past an adapter's rank
- * plays no part, whatever it is.  base is what hawq_linear_w4 left, for instance; y may be base, with its stride (HAWQ_ERR_SHAPE
+ * float32 [n_adapters].  A row whose adapter is not one of 0..n_adapters - 1 (as -1), or has rank 0, gets base as it is.  What lies past an
+ * adapter's rank plays no part, whatever it is.  base is what hawq_linear_w4 left, for instance; y may be base, with its stride (HAWQ_ERR_SHAPE
  * otherwise), no other overlap.  Rows of one adapter share its reading where they lie near one another.
- * The inner sums are kept in 32 bits (or as two parts of T that hold 15 bits or more); the result is rounded once.
+ * The inner sums are kept in 32 bits and meet b as two parts of T that hold 15 bits (bf16) or 21 (f16, of the row's largest) or more; the
+ * outer sums have 32 bits, and the result is rounded once.  M, N and K up to 2^31 - 4096, max_rank up to 2^16.
  * workspace: device memory of hawq_adapters_workspace_bytes(desc) bytes (0 for an invalid desc), 16-byte aligned, scratch.
  */
 typedef struct {

@@ -10,6 +10,10 @@
 // h stays at 32 bits' worth: the matrix instruction takes 16-bit operands, so h goes in as two parts, hi = T(h) and lo = T(h - hi), which
 // hold 2^-18 of it (bf16) or 2^-22 (f16, after a power of two for each row that brings its largest to 2^13: a half neither overflows nor
 // loses lo's last bits there).  The second product costs nothing beside the bytes of y.
+//
+// Few rows are bound by two launches and the loads' latency (one row of 768 x 768 7.7 us, 48 rows of 4096 x 4096 over twelve adapters 15), many
+// by bytes on their way: 5003 rows of 4096 x 4096 take 55 us, of which the inner product is 22 (48 MB, more of them under way would need more
+// registers than 336 of a lane) and the outer one 31 (98 MB and the inner sums of each part once for 512 outputs, 160 MB of L2's).
 #include "lm.h"
 #include "lm_launch.h"
 
@@ -71,7 +75,7 @@ __device__ __forceinline__ typename T::v8 load8(const typename T::elem *p, int k
 
 // Ranks rb .. rb + 16 NT - 1 of the rows' inner sums over the workgroup's part of K.
 template <class T, int MT, int NT, bool VECTOR>
-__device__ __forceinline__ void inner_tile(const AdaptersArgs &a, int m0, int id, int rank, int rb, uint64_t rows, int first, int stride, float *h, float *red) {
+__device__ __forceinline__ void inner_tile(const AdaptersArgs &a, int m0, int id, int rank, int rb, uint64_t rows, int first, int sharers, float *h, float *red) {
     typedef typename T::elem E;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, c = lane >> 4;
     const E *x[MT], *row[NT];
@@ -95,20 +99,21 @@ __device__ __forceinline__ void inner_tile(const AdaptersArgs &a, int m0, int id
             for (int i = 0; i < MT; ++i)
                 for (int t = 0; t < NT; ++t) acc[i][t] = T::mfma16(g.a[t][s], g.x[i][s], acc[i][t]);
     };
-    const int last = (a.K + kSteps - 1) / kSteps;
-    int step = first + wave;
-    if (step < last) {
+    // (a wave's steps side by side: 55 us for 5003 rows over four adapters, one apart from the next by all waves 57)
+    const int all = (a.K + kSteps - 1) / kSteps, each = (all + sharers - 1) / sharers;
+    const int64_t begin = (int64_t)(first + wave) * each;
+    if (begin < all) {
+        int step = (int)begin;
+        const int last = min(all, step + each);
         Stage even, odd;
         load(step, even);
         for (;;) {
-            load(min(step + stride, last - 1), odd);
+            load(min(step + 1, last - 1), odd);
             use(even);
-            step += stride;
-            if (step >= last) break;
-            load(min(step + stride, last - 1), even);
+            if (++step >= last) break;
+            load(min(step + 1, last - 1), even);
             use(odd);
-            step += stride;
-            if (step >= last) break;
+            if (++step >= last) break;
         }
     }
     constexpr int kRow = 16 * NT + 4;

