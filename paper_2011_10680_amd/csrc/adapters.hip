@@ -11,7 +11,7 @@
 // hold 2^-18 of it (bf16) or 2^-22 (f16, after a power of two for each row that brings its largest to 2^13: a half neither overflows nor
 // loses lo's last bits there).  The second product costs nothing beside the bytes of y.
 //
-// Few rows are bound by two launches and the loads' latency (one row of 768 x 768 7.7 us, 48 rows of 4096 x 4096 over twelve adapters 15), many
+// Few rows are bound by two launches and the loads' latency (one row of 768 x 256 7.7 us, 48 rows of 6144 x 4096 over twelve adapters 15), many
 // by bytes on their way: 5003 rows of 4096 x 4096 take 55 us, of which the inner product is 22 (48 MB, more of them under way would need more
 // registers than 336 of a lane) and the outer one 31 (98 MB and the inner sums of each part once for 512 outputs, 160 MB of L2's).
 #include "lm.h"
