@@ -138,15 +138,10 @@ struct Row {
         }
     }
 
-    // The tokens v0 .. v0 + n - 1 by words of their own, count[n], and where the list is long place[n]; both with three words to spare.
+    // The tokens v0 .. v0 + n - 1 by words of their own, count[n], and where the list is long place[n], cleared before and seen by all.
     // Whoever counted a token takes its word away afterwards: the first one writes the token's logit again.
     __device__ __forceinline__ void settle(int v0, int n, uint32_t *count, uint32_t *place) const {
         const bool places = biases > kFewBiases;
-        for (int i = threadIdx.x; i < (n + 3) / 4; i += THREADS) {
-            ((v4u *)count)[i] = v4u{0, 0, 0, 0};
-            if (places) ((v4u *)place)[i] = v4u{0, 0, 0, 0};
-        }
-        __syncthreads();
         each([&](int32_t token, int entry, bool written) {
             const uint32_t at = (uint32_t)token - (uint32_t)v0;
             if (at >= (uint32_t)n) return;
@@ -185,9 +180,14 @@ struct Row {
             for (int i = 0; i < 4; ++i) token[i] = i0 < THREADS ? head[i] : past[min(i0 + i * THREADS, len - 1)];
             take(token);
         }
-        __syncthreads();
     }
 };
+
+// n words, a multiple of four
+template <int THREADS>
+__device__ __forceinline__ void clear(uint32_t *words, int n) {
+    for (int i = threadIdx.x; i < n / 4; i += THREADS) ((v4u *)words)[i] = v4u{0, 0, 0, 0};
+}
 
 // IN_PLACE: y is x, and what does not change is neither read nor written.  WORDS: tokens are counted here, too.
 template <class T, bool IN_PLACE, bool WORDS>
@@ -213,6 +213,7 @@ __global__ __launch_bounds__(kPartThreads) void logits_part(LogitsArgs a, int pa
     if (b < 0) return;
     Row<T, kPartThreads> row;
     row.load(a, t, b);
+    if (WORDS) clear<kPartThreads>(words, part + 16);
     const uint32_t *const allowed = row.allowed;
     auto copy = [&](int k, Eight d) {
         const int at = 8 * k - off;              // of the eight's first element in the part
@@ -253,9 +254,21 @@ __global__ __launch_bounds__(kPartThreads) void logits_part(LogitsArgs a, int pa
         }
     }
     if (!WORDS || (!row.counts && row.biases == 0)) return;
-    __syncthreads();                             // (what is written again comes after what was copied)
-    const int half = row.biases > kFewBiases ? (part / 2 + 3) & ~3 : part;       // a long list's places share the words
-    for (int first = 0; first < n; first += half) row.settle(v0 + first, min(half, n - first), words, words + half);
+    // Words are cleared for all.  (__syncthreads would wait for the copy here, too, which has until the tokens are counted: it is what comes between
+    // counting and writing again.)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int half = row.biases > kFewBiases ? part / 2 + 4 : part;              // a long list's places share the words
+    for (int first = 0; first < n; first += half) {
+        if (first > 0) {
+            __syncthreads();
+            clear<kPartThreads>(words, part + 16);
+            __syncthreads();
+        }
+        row.settle(v0 + first, min(half, n - first), words, words + half);
+    }
 }
 
 // The tokens of one row, behind its copy.
@@ -271,16 +284,19 @@ __global__ __launch_bounds__(kRowThreads) void logits_row(LogitsArgs a) {
     const int64_t tokens = (int64_t)row.len + row.seen + row.biases;
     if (tokens == 0) return;
     if (tokens > kMostHashed || row.biases > kFewBiases) {
-        for (int64_t v = 0; v < a.vocab; v += kSlots) row.settle((int)v, (int)min((int64_t)kSlots, a.vocab - v), words, words + kSlots);
+        for (int64_t v = 0; v < a.vocab; v += kSlots) {
+            __syncthreads();
+            clear<kRowThreads>(words, 2 * kSlots);
+            __syncthreads();
+            row.settle((int)v, (int)min((int64_t)kSlots, a.vocab - v), words, words + kSlots);
+        }
         return;
     }
     // slots of a token and a word, half as many again as tokens or more: 4096, 8192 or 16384
     uint32_t *const key = words, *const count = words + kSlots;
     const int bits = tokens <= 2700 ? 12 : tokens <= 5400 ? 13 : 14, slots = 1 << bits;
-    for (int i = threadIdx.x; i < slots / 4; i += kRowThreads) {
-        ((v4u *)key)[i] = v4u{0, 0, 0, 0};
-        ((v4u *)count)[i] = v4u{0, 0, 0, 0};
-    }
+    clear<kRowThreads>(key, slots);
+    clear<kRowThreads>(count, slots);
     __syncthreads();
     row.each([&](int32_t token, int entry, bool written) {
         if ((uint32_t)token >= (uint32_t)a.vocab) return;
