@@ -12,8 +12,9 @@
 // loses lo's last bits there).  The second product costs nothing beside the bytes of y.
 //
 // Few rows are bound by two launches and the loads' latency (one row of 768 x 256 7.7 us, 48 rows of 6144 x 4096 over twelve adapters 15), many
-// by bytes on their way: 5003 rows of 4096 x 4096 take 55 us, of which the inner product is 22 (48 MB, more of them under way would need more
-// registers than 336 of a lane) and the outer one 31 (98 MB and the inner sums of each part once for 512 outputs, 160 MB of L2's).
+// by bytes on their way: 5003 rows of 4096 x 4096 take 55 us from the caches and 70 from memory, the inner product 26 of them (47 MB; a lane
+// has 336 registers, so that a compute unit has four waves with two steps each under way) and the outer one 31 (120 MB, 3.9 TB/s, 32 MB of them the
+// inner sums' parts, which every XCD reads; a tile's outputs on one XCD read fewer and took 33).
 #include "lm.h"
 #include "lm_launch.h"
 
