@@ -16,7 +16,8 @@
 // Bound by the two pipes: 2049 rows of 8192 x 4096 (bf16, groups of 128, zero points) take 273 us, 1010 TFLOP/s, of which the sums of x are 5 and
 // the last row's launch 13; the matrix pipe works half of the kernel's time, the vector pipe 0.57.  A library's bf16 product of 8192 cubed reaches
 // 1210 to 1485 here.  On the way: the form for few rows 1297 us, a tile of 128 x 128 541, three steps under way and scales in LDS 385, wider
-// tiles of a wave and a group of 128 scaled once 366, waves in turn 313, the last row by the form for few 273.  13 rows of 12288 x 4096 take 17.6 us (55 MB of codes, scales and zero points: 10.7 at the rate of a large copy).
+// tiles of a wave and a group of 128 scaled once 366, waves in turn 313, the last row by the form for few 273.
+// 13 rows of 12288 x 4096 take 17.6 us (55 MB of codes, scales and zero points: 10.7 at the rate of a large copy).
 #include "linear_w4.h"
 
 namespace hawq {

@@ -10,8 +10,9 @@
 // so that the row's tokens are read once.  Rows with more tokens or longer lists than that holds go part by part there, too.
 //
 // Bound by the logits' bytes for many rows, by a chain of loads (request, lengths, tokens, logits) and a launch for few.  Measured: 256 x 128001
-// 43 us, of which the copy alone is 27 (4.9 TB/s) and the tokens 13; 171 x 64000 18; one row of 32000 6, twice an empty launch.  Words checked in
-// order instead of by token, in one launch: 256 x 128001 64 us and more, the copy's loop no longer in the instruction cache.
+// 57 us from memory, 43 from the caches, of which the copy is 27 (4.9 TB/s) and the tokens 16; 171 x 64000 27.5 and 18; one row of 32000 6, twice
+// an empty launch.  Words checked in order instead of by token, in one launch: 256 x 128001 64 us and more from the caches, the copy's loop no
+// longer in the instruction cache.
 #include "lm.h"
 #include "lm_launch.h"
 
@@ -300,11 +301,15 @@ __global__ __launch_bounds__(kRowThreads) void logits_row(LogitsArgs a) {
     __syncthreads();
     row.each([&](int32_t token, int entry, bool written) {
         if ((uint32_t)token >= (uint32_t)a.vocab) return;
-        uint32_t at = (uint32_t)token * 2654435761u >> (32 - bits);
-        for (;;) {                               // (ends: there are more slots than tokens)
+        const uint32_t product = (uint32_t)token * 2654435761u;      // (2^32 by the golden ratio)
+        // (odd steps reach every slot, of which there are more than tokens; steps of a token's own: the slots beside one another that a history
+        // may have been made for fill up no faster than others)
+        uint32_t at = product >> (32 - bits);
+        const uint32_t on = product >> 6 | 1u;
+        for (;;) {
             const uint32_t had = atomicCAS(key + at, 0u, (uint32_t)token + 1);
             if (had == 0 || had == (uint32_t)token + 1) break;
-            at = (at + 1) & (slots - 1);
+            at = (at + on) & (slots - 1);
         }
         if (entry >= 0) {
             highest(count + at, (uint32_t)entry + 1);

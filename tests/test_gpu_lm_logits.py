@@ -201,3 +201,14 @@ def test_many_logits():
     """Past 2^24 logits, with drafts, masks, short and long lists, and rows behind the last request."""
     _run([5] * 25 + [4], 131073, [40 * i for i in range(26)], "bf16", biases=60, masks=20, pad=3, behind=1, seed=1)
     _run([1] * 33, 600001, [1000] * 32 + [11000], "f16", biases=300, masks=5, in_place=True, few=3000, seed=2)
+
+
+@pytest.mark.parametrize("seed", [1, 2])
+def test_histories_of_neighbouring_hashes(seed):
+    """Tokens whose product with the hash's factor has small upper bits: all begin their search in a few places beside one another."""
+    V = 131072
+    order = np.argsort((np.arange(V, dtype=np.uint64) * 2654435761 & 0xFFFFFFFF) >> 18, kind="stable").astype(np.int32)
+    def change(i):
+        i["past"][:] = order[np.random.default_rng(seed).integers(0, 9000, size=i["past"].shape)]
+        i["past"][0, :9000] = order[:9000]
+    _run([1, 1], V, [9900, 4000], "bf16", biases=20, in_place=True, seed=seed, change=change)
