@@ -149,6 +149,21 @@ __global__ __launch_bounds__(64 * waves_of(MT)) void inner(AdaptersArgs a, int s
     });
 }
 
+// A sum over the ranks as the formula stands.  That of the two parts of h differs from it where b is infinite (the second part may be 0, or of
+// the other sign), and where h is a number of 32 bits that rounds to an infinite one of the type.
+template <class T>
+__device__ __forceinline__ float plain_outer(const AdaptersArgs &a, int m, const typename T::elem *b, int rank, int splits) {
+    double v = 0;
+#pragma unroll 1
+    for (int j = 0; j < rank; ++j) {
+        const float *p = a.h + (int64_t)m * a.max_rank + j;
+        float h = 0;
+        for (int s = 0; s < splits; ++s) h += p[(int64_t)s * a.M * a.max_rank];
+        v += (double)(float)b[j] * (double)h;
+    }
+    return (float)v;
+}
+
 // 64 outputs of a wave at a time: tile t of its product has outputs n0 + 16 c + 4 t + e where the instruction has rows 4 c + e, so that a lane
 // ends with 16 outputs that lie side by side.
 template <class T, int MT, bool VECTOR, bool ROWS>
@@ -251,11 +266,14 @@ __global__ __launch_bounds__(256) void outer(AdaptersArgs a, int slots, int spli
             for (int i = 0; i < MT; ++i) {
                 const int m = m0 + 16 * i + r;
                 if (!(rows >> (16 * i + r) & 1)) continue;
+                float none = 0;                          // 0, or no number where a sum is not finite
+                for (int t = 0; t < 4; ++t)
+                    for (int e = 0; e < 4; ++e) none = fmaf(acc[i][t][e], 0.f, none);
                 const E *base = (const E *)a.base + m * a.base_stride + n;
                 E *y = (E *)a.y + m * a.y_stride + n;
                 const float up = std::is_same<T, F16>::value && id >= 0 ? unit[16 * i + r] : 1.f;
                 auto sum = [&](E v, float add) { return id >= 0 ? (E)((float)v + scale * add * up) : v; };
-                if (ROWS && n + 16 <= a.N) {
+                if (ROWS && n + 16 <= a.N && none == 0) {
                     for (int q = 0; q < 2; ++q) {
                         typename T::v8 v = ahead[ROWS ? i : 0][q];
                         for (int e = 0; e < 8; ++e) v[e] = sum(v[e], acc[i][2 * q + (e >> 2)][e & 3]);
@@ -266,6 +284,7 @@ __global__ __launch_bounds__(256) void outer(AdaptersArgs a, int slots, int spli
                         float add = 0;
                         for (int t = 0; t < 4; ++t)
                             for (int f = 0; f < 4; ++f) add = e == 4 * t + f ? acc[i][t][f] : add;
+                        if (!(fabsf(add) < INFINITY)) add = plain_outer<T>(a, m, b + (n + e) * a.b_row, rank, splits) / up;
                         y[e] = sum(base[e], add);
                     }
                 }
