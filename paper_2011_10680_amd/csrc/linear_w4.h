@@ -85,18 +85,23 @@ __device__ __forceinline__ double plain_output(const LinearW4Args &a, int m, int
     return v;
 }
 
-// exp(v): v log2(e) as a product and what rounding it left out (2 units in the last place; one of 30 alone would be off by 20)
-__device__ __forceinline__ float exp_of(float v) {
-    const float t = v * 1.44269504f, rest = fmaf(v, 1.92596303e-8f, fmaf(v, 1.44269504f, -t));
-    const float e = __builtin_amdgcn_exp2f(t);
-    return fabsf(t) < 126.f ? fmaf(e, rest * 0.693147181f, e) : e;
+// g / (1 + exp(-t)) by exp(-|t|), which is 1 at most.  Its argument is a product with log2(e) and what rounding that left out (2 units in the last
+// place; the product alone would be off by 30).  The instruction has no results below 2^-126, where g times it still is a number: such ones are taken
+// times 2^64, and 1 + exp(-|t|) is 1 there.
+__device__ __forceinline__ float gate_of(float g, float t) {
+    const float v = -fabsf(t), p = v * 1.44269504f, rest = fmaf(v, 1.92596303e-8f, fmaf(v, 1.44269504f, -p));
+    const bool far = p < -64.f;
+    float e = __builtin_amdgcn_exp2f(far ? p + 64.f : p);
+    e = p > -256.f ? fmaf(e, rest * 0.693147181f, e) : e;
+    const float r = __builtin_amdgcn_rcpf(far ? 1.f : 1.f + e);
+    return t < 0 ? g * e * (far ? 0x1p-64f : r) : g * r;
 }
 
 // The gate's activation.  The normal distribution's tail is taken by itself, not as a difference from 1.
 __device__ __forceinline__ float activated(float g, int kind) {
-    if (kind == HAWQ_SILU) return g * __builtin_amdgcn_rcpf(1.f + exp_of(-g));
+    if (kind == HAWQ_SILU) return gate_of(g, g);
     if (kind == HAWQ_GELU) return 0.5f * g * erfcf(g * -0.70710678118654752f);
-    if (kind == HAWQ_GELU_TANH) return g * __builtin_amdgcn_rcpf(1.f + exp_of(-1.5957691216057308f * (g + 0.044715f * g * g * g)));      // (1 + tanh t) / 2 = 1 / (1 + exp(-2 t))
+    if (kind == HAWQ_GELU_TANH) return gate_of(g, 1.5957691216057308f * (g + 0.044715f * g * g * g));      // (1 + tanh(t / 2)) / 2 = 1 / (1 + exp(-t))
     return g > 0.f || g != g ? g : 0.f;
 }
 
