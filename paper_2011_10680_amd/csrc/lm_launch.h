@@ -27,4 +27,13 @@ constexpr int first_chunks(float all, unsigned workgroups, int waves) {
     return (int)(each < 0x1p27f ? each : 0x1p27f) / waves * waves + waves;
 }
 
+// Tokens of the vocabulary to a workgroup of the logits' copy: 16384, fewer where that gives the 256 compute units less than four workgroups each.
+// And how many such parts there are.
+inline int64_t logits_parts(int32_t vocab, int part) { return ((int64_t)vocab + part - 1) / part; }
+inline int logits_part_of(int32_t total, int32_t vocab) {
+    int part = 16384;
+    while (part > 1024 && total * logits_parts(vocab, part) < 1024) part /= 2;
+    return part;
+}
+
 }  // namespace hawq

@@ -333,11 +333,9 @@ hawq_status launch(const LogitsArgs &a, hipStream_t s) {
     const bool counted = a.penalties || a.n_bias > 0, copied = !IN_PLACE || a.n_allowed > 0;
     const bool apart = counted && (!copied || (int64_t)a.total * a.vocab >= kApart);
     if (copied) {
-        // parts of 16384 tokens, smaller ones where that gives the 256 compute units less than four each
-        int part = 16384;
-        while (part > 1024 && (int64_t)a.total * ((a.vocab + part - 1) / part) < 1024) part /= 2;
+        const int part = logits_part_of(a.total, a.vocab);
         const int64_t along = a.total < kMostAlong ? a.total : kMostAlong;
-        const dim3 grid((unsigned)(((int64_t)a.vocab + part - 1) / part), (unsigned)along, (unsigned)((a.total + along - 1) / along));
+        const dim3 grid((unsigned)logits_parts(a.vocab, part), (unsigned)along, (unsigned)((a.total + along - 1) / along));
         if (counted && !apart) logits_part<T, IN_PLACE, true><<<grid, kPartThreads, (size_t)(part + 16) * 4, s>>>(a, part);
         else logits_part<T, IN_PLACE, false><<<grid, kPartThreads, 0, s>>>(a, part);
         const hawq_status st = check_launch();
