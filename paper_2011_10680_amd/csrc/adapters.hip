@@ -155,7 +155,7 @@ template <class T>
 __device__ __forceinline__ float plain_outer(const AdaptersArgs &a, int m, const typename T::elem *b, int rank, int splits) {
     double v = 0;
 #pragma unroll 1
-    for (int j = 0; j < rank; ++j) {
+    for (int j = 0; j < rank && v == v; ++j) {      // (no number stays none)
         const float *p = a.h + (int64_t)m * a.max_rank + j;
         float h = 0;
         for (int s = 0; s < splits; ++s) h += p[(int64_t)s * a.M * a.max_rank];
