@@ -560,6 +560,8 @@ hawq_status hawq_rotary(const hawq_rotary_desc *desc, const void *q, const void 
  * by 5 10^-7; without a mean by 10^-6 and 3 10^-7.
  * act:  HAWQ_SILU g / (1 + exp(-g));  HAWQ_GELU g Phi(g), Phi the normal distribution's;  HAWQ_GELU_TANH its approximation
  * g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3)));  HAWQ_RELU max(g, 0).
+ * Prompts' form takes K a multiple of 32 up to 2^16, x_stride a multiple of 8 up to 2^22, up to 2^29 rows, and x and w at multiples of 16 bytes; other
+ * calls are served as few rows are, 16 to 64 at a time, several times slower for a whole prompt.
  * workspace: device memory of hawq_gated_w4_workspace_bytes(desc) bytes (0 for few rows or an invalid desc), 16-byte aligned, scratch.
  */
 typedef enum { HAWQ_SILU = 0, HAWQ_GELU = 1, HAWQ_GELU_TANH = 2, HAWQ_RELU = 3 } hawq_activation;
@@ -614,7 +616,9 @@ hawq_status hawq_adapters(const hawq_adapters_desc *desc, const void *x, const v
  * (a number outside 0..n_allowed - 1, as -1: everything is allowed); allowed_row == NULL: row t's is the t-th, n_allowed >= total.  A mask
  * may leave a row empty: all of it is -infinity then.  n_bias == 0 and n_allowed == 0: none, their pointers are not looked at.
  * y may be x, with its stride (HAWQ_ERR_SHAPE otherwise); only what changes is then written.  No other overlap.
- * Fewer than 2^23 rows, and a past_stride below that; up to 2^31 - 4096 tokens in the vocabulary.
+ * Fewer than 2^23 rows, and a past_stride below that; up to 2^31 - 4096 tokens in the vocabulary.  A row's tokens are read twice for every part of
+ * the vocabulary (1024 to 16384 tokens) by the workgroup that copies it; in place without masks, and from 2^24 logits on, once in all for up to 10000 tokens
+ * and 127 biases, with more of either twice for every 16384 of the vocabulary by one workgroup.
  */
 typedef struct {
     int32_t n_seqs, total, vocab;

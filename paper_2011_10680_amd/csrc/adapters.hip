@@ -9,12 +9,14 @@
 //
 // h stays at 32 bits' worth: the matrix instruction takes 16-bit operands, so h goes in as two parts, hi = T(h) and lo = T(h - hi), which
 // hold 2^-18 of it (bf16) or 2^-22 (f16, after a power of two for each row that brings its largest to 2^13: a half neither overflows nor
-// loses lo's last bits there).  The second product costs nothing beside the bytes of y.
+// loses lo's last bits there).  The second product costs nothing beside the bytes of y.  A sum that the two parts leave infinite or no number is
+// taken once more from h itself, by its own lane (5003 rows of NaN 0.5 ms, of infinities 1.3).
 //
 // Few rows are bound by two launches and the loads' latency (one row of 768 x 256 7.7 us, 48 rows of 6144 x 4096 over twelve adapters 15), many
-// by bytes on their way: 5003 rows of 4096 x 4096 take 55 us from the caches and 70 from memory, the inner product 26 of them (47 MB; a lane
-// has 336 registers, so that a compute unit has four waves with two steps each under way) and the outer one 31 (120 MB, 3.9 TB/s, 32 MB of them the
-// inner sums' parts, which every XCD reads; a tile's outputs on one XCD read fewer and took 33).
+// by bytes on their way: 5003 rows of 4096 x 4096 take 55 us from the caches and 70 to 74 from memory, the inner product 26 of them (47 MB; a lane
+// has 312 registers, 332 where elements are read one by one, so that a compute unit has four waves; what lies past K is put to zero where it is
+// loaded, so that a step's loads have landed before the products of the step in front of it end) and the outer one 31 (120 MB, 3.9 TB/s, 32 MB of
+// them the inner sums' parts, one read after the other by every XCD; a tile's outputs on one XCD read fewer and took 33).
 #include "lm.h"
 #include "lm_launch.h"
 

@@ -10,7 +10,7 @@
 // groups.  It costs the matrix pipe a sixteenth (groups of 128) to a quarter (32); subtracted by the vector pipe it would cost that as much as the scaling.
 // It is taken off first, for 64 groups at a time, so that a running sum is as large as it and rounds to 2^-24 of that: with x of mean 3 and spread 1 the sums
 // are off by 8 10^-6 (K = 4096, groups of 128), 1.6 10^-5 (groups of 32) or 2 10^-5 (K = 65536) of their size, where the form for few rows has 3 to 5 10^-7;
-// under the rounding of the type, 2^-11 or 2^-8.  Group by group it would need the sums of x beside the steps' tiles in LDS, which are 147 of 160 KB.
+// under the rounding of the type, 2^-11 or 2^-8.  Group by group it would need the sums of x beside the steps' tiles in LDS, which are 146 of 160 KB.
 //
 // x comes into LDS by direct loads, 64 inputs at a time in four arrays in turn, weights 128 inputs at a time in two; pieces are swizzled so that
 // the operand reads are free of bank conflicts.  Two exchanges between a wave's halves give each operand register eight consecutive inputs.  The

@@ -7,7 +7,8 @@
 //
 // Few logits go through one launch: a workgroup copies a part of the vocabulary and counts the tokens that fall into it, words lying by token.
 // Many go through two: a copy that waits for nothing but the mask, and a workgroup for each row, whose words lie by a hash of the token,
-// so that the row's tokens are read once.  Rows with more tokens or longer lists than that holds go part by part there, too.
+// so that the row's tokens are read once.  Rows with more tokens or longer lists than that holds go part by part there, too, all parts in one
+// workgroup (a row of 128001 in place: 9999 tokens 20 us, 10001 50, 131072 465; by a workgroup for each part, where it is copied, 11, 11 and 93).
 //
 // Bound by the logits' bytes for many rows, by a chain of loads (request, lengths, tokens, logits) and a launch for few.  Measured: 256 x 128001
 // 57 us from memory, 43 from the caches, of which the copy is 27 (4.9 TB/s) and the tokens 16; 171 x 64000 27.5 and 18; one row of 32000 6, twice
@@ -22,7 +23,7 @@ namespace {
 
 constexpr uint32_t kOccurred = 0x80000000u, kPlaces = 0x7F000000u, kListed = 1u << 24, kCount = 0x00FFFFFFu;
 constexpr int kFewBiases = 127;                  // whose places a word holds
-constexpr int kPartThreads = 512, kAhead = 4;    // eights of a thread on their way while the request is looked for
+constexpr int kPartThreads = 512, kAhead = 4;    // eights of a thread that are loaded before the request is looked for, one after the other (each in a branch)
 // Logits from which tokens are counted in a launch of their own: 171 x 64000 take 18.5 us in one launch and 20.9 in two, 256 x 128001 61 and 43.
 constexpr int64_t kApart = 1 << 24;
 constexpr int kRowThreads = 1024, kSlots = 16384, kMostHashed = 10000;
@@ -109,7 +110,7 @@ struct Row {
     __device__ __forceinline__ void each(F &&f) const {
         for (int i = threadIdx.x; i < biases; i += THREADS) f(i < THREADS ? listed : bias_ids[i], i, false);
         for (int i = threadIdx.x; i < seen; i += THREADS) f(sees >> (i & 63) & 1 ? i < THREADS ? draft : drafts[i] : -1, -1, true);      // (-1 is no token)
-        // (four on their way at a time)
+        // (four tokens on their way at a time)
         for (int i0 = threadIdx.x; i0 < len; i0 += 4 * THREADS) {
             int32_t token[4];
             for (int i = 0; i < 4; ++i) token[i] = i0 < THREADS ? head[i] : past[min(i0 + i * THREADS, len - 1)];
@@ -118,7 +119,8 @@ struct Row {
         }
     }
 
-    // the logits of tokens v[i] with words c[i], 0: none; place: entries of the list and 1, 0: not in it
+    // the logits of tokens v[i] with words c[i], 0: none; place: entries of the list and 1, 0: not in it (in a row with a mask the mask's words are
+    // read in branches, one after the other)
     template <int N>
     __device__ __forceinline__ void again(const int (&v)[N], const uint32_t (&c)[N], const uint32_t (&place)[N]) const {
         E l[N];
